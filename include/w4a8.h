@@ -480,6 +480,90 @@ int w4a8_forward_host(const void* x_host_bf16, int64_t M, const uint8_t* weights
                       size_t workspace_bytes, void* stream);
 
 /*
+ * FP8 layers with a scale per block of 128, for the layers of a model that stay in 8 bits beside its W4A8 ones (checkpoints
+ * with one scale per 128 x 128 weights), and mixture-of-experts blocks made of them.  The paper quantizes activations per token
+ * (Eq. 13) and weights per channel or tensor (Eq. 6); here both definitions are applied per block of 128 columns:
+ *       X8     E4M3  [M][ldx8], s_x FP32 [M][lds]               one scale per token and 128 columns
+ *       W8     E4M3  [N][ldw],  s_w FP32 [ceil(N/128)][ceil(K/128)]   one scale per 128 x 128 weights
+ * K % 16 == 0 and N % 16 == 0; the last blocks may be short.  Where a tensor has a leading dimension, values behind a row's last
+ * column are neither read nor written.  No call below needs memory of its own except w4a8_route_experts, whose workspace needs no
+ * preparation; nothing is kept between calls, and calls on different streams may overlap as long as their outputs (and the
+ * workspaces of w4a8_route_experts) differ.
+ */
+
+/*
+ * Activation quantization, Eq. 13 per token and block of 128 columns (the last one may be shorter):
+ *   amax = max |x| over the block;  s_x = max(amax, 2^-100) / 448 (fp32 division; 1 when the block is all zero);
+ *   X8 = nearest_E4M3( x * (448 / max(amax, 2^-100)) )  -- one fp32 multiply, as w4a8_quantize_act.
+ * input_kind W4A8_CHAIN_INPUT_SILU_MUL: x_bf16 holds gate (K columns) and up (K columns behind them), x = silu(gate) * up in
+ * FP32 -- not rounded to BF16 in between as in w4a8_silu_mul_quantize.  NaN stays NaN; a block with an infinity has s_x = inf
+ * and NaN in its place.
+ * slots (int32 [M][top_k], contiguous; NULL with top_k = 0): token m's row is written to the rows slots[m][0..top_k) of x8 and
+ * s_x, as w4a8_route_experts gives them; entries outside [0, rows) are skipped, rows that no entry names are left as they were
+ * (an entry must not be there twice).  NULL: token m is row m, rows >= M, and rows behind M are left as they were.
+ * ldx % 8 == 0; ldx8 % 16 == 0.
+ */
+int w4a8_quantize_act_blocks(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, int input_kind, const int32_t* slots,
+                             int top_k, uint8_t* x8, int64_t rows, int64_t ldx8, float* s_x, int64_t lds, void* stream);
+
+/*
+ * Linear layer with block scales:
+ *   Y[m][n] = sum_b s_x[m][b] * s_w[n / 128][b] * ( sum of X8[m][k] * W8[n][k] over the columns k of block b )
+ * Products of a block are accumulated in FP32 by the tensor cores, blocks in FP32; rounded to BF16 (out_dtype 0) or kept in
+ * FP32 (1).  Any M; results repeat bit for bit.  ldx8 % 16 == 0, ldw % 16 == 0, Y 16-byte aligned.
+ */
+int w4a8_linear_fp8_blocks(const uint8_t* x8, int64_t ldx8, const float* s_x, int64_t lds, int64_t M, const uint8_t* w8,
+                           int64_t ldw, const float* s_w, int64_t N, int64_t K, void* y, int64_t ldy, int out_dtype,
+                           void* stream);
+
+/*
+ * The same for `experts` layers of one shape at once (at most 512): row r of X8 is multiplied with the weights of the expert e
+ * with offsets[e] <= r < offsets[e + 1] (int32 [experts + 1] on the device, as w4a8_route_experts gives them).  w8 holds
+ * the experts w_stride bytes apart (w_stride % 16 == 0), s_w [experts][ceil(N/128)][ceil(K/128)].  Weights of experts without
+ * rows are not read.  rows is the height of X8 and Y: rows of Y outside [offsets[0], offsets[experts]) are left as they were.
+ * Offsets that descend or lie outside [0, rows] are taken as the highest before them and into that range.
+ */
+int w4a8_linear_fp8_experts(const uint8_t* x8, int64_t ldx8, const float* s_x, int64_t lds, int64_t rows,
+                            const int32_t* offsets, int64_t experts, const uint8_t* w8, int64_t ldw, int64_t w_stride,
+                            const float* s_w, int64_t N, int64_t K, void* y, int64_t ldy, int out_dtype, void* stream);
+
+/*
+ * Routing of M tokens to top_k of `experts` experts (at most 512, top_k at most 32) from router logits (BF16 or FP32 by
+ * logits_dtype, [M][ldl]):
+ *   score = softmax of the token's logits, or their sigmoid;  key = score + bias (bias FP32 [experts] or NULL; it serves the
+ *   choice alone);
+ *   groups > 1 (at most 32, dividing experts): a group's key is the sum of its group_best (1 or 2) highest keys, or of all of a
+ *   smaller group; only experts of the top_groups groups of highest key can be chosen;
+ *   the top_k experts of highest key are chosen in descending order.  Equal keys: the lower index first, groups and experts.
+ *   weights = score, divided by the sum of the chosen scores (renormalize = 1; 0 where that sum is 0), times scale.
+ * Keys are compared as FP64 values (without a bias and with group_best = 1 as the logits themselves, which have their order).
+ * Experts whose logit is NaN or -inf, or whose bias is, cannot be chosen (a NaN logit counts as -inf in the softmax); a group with
+ * fewer than group_best experts that can be comes last.  A token with fewer than top_k experts has id -1, weight 0 and slot
+ * -1 behind them: a row of -inf goes to no expert.
+ * Outputs: ids int32 and weights FP32 [M][top_k]; and the rows' order by expert: offsets int32 [experts + 1] (row offsets of the
+ * experts, offsets[experts] = rows in all) and slots int32 [M][top_k], the row of each choice -- within an expert in ascending
+ * order of the tokens.  workspace: w4a8_route_experts_workspace_bytes(M, experts) bytes, 4-byte aligned, scratch (at most a
+ * count per expert and sixteen tokens; NULL where 0).
+ */
+#define W4A8_SCORE_SOFTMAX 0
+#define W4A8_SCORE_SIGMOID 1
+size_t w4a8_route_experts_workspace_bytes(int64_t M, int64_t experts);
+int w4a8_route_experts(const void* logits, int logits_dtype, int64_t M, int64_t ldl, int64_t experts, int top_k, int score,
+                       const float* bias, int groups, int top_groups, int group_best, int renormalize, float scale,
+                       int32_t* ids, float* weights, int32_t* offsets, int32_t* slots, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Weighted sum of the experts' outputs: out[m] = add[m] + sum_j weights[m][j] * y[slots[m][j]], FP32 sums in ascending order
+ * of j, rounded once to out_dtype.  y [rows][ldy] in y_dtype; slots and weights [M][top_k], contiguous; slots outside [0, rows)
+ * add nothing (their weights and no row of y are looked at); add (out_dtype, [M][ldadd]) may be NULL and may be out itself.
+ * N % 16 == 0; rows of y, add and out 16-byte aligned.
+ */
+int w4a8_combine_experts(const void* y, int y_dtype, int64_t rows, int64_t ldy, const int32_t* slots, const float* weights,
+                         int64_t M, int top_k, int64_t N, const void* add, int64_t ldadd, void* out, int64_t ldo,
+                         int out_dtype, void* stream);
+
+/*
  * Reads and clears the device-side status word (synchronises the device).  *flags receives a
  * bit mask: bit 0 = a bounded wait inside a kernel gave up; bit 1 = w4a8_prepack_weight met a
  * code its target format cannot hold; the others are unused.  Bit 0 means that the outputs of some

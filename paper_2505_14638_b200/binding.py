@@ -36,10 +36,13 @@ EXPORTS = (
     "w4a8_forward_host", "w4a8_query_device_status", "w4a8_launch_count", "w4a8_status_string",
     "w4a8_linear_chain", "w4a8_linear_chain_workspace_bytes", "w4a8_selftest_bounded_wait",
     "w4a8_host_buffer_device_pointer",
+    "w4a8_quantize_act_blocks", "w4a8_linear_fp8_blocks", "w4a8_linear_fp8_experts",
+    "w4a8_route_experts", "w4a8_route_experts_workspace_bytes", "w4a8_combine_experts",
 )
 
 CHAIN_INPUT_PLAIN, CHAIN_INPUT_SILU_MUL = 0, 1
 CHAIN_MAX_PROBLEMS, CHAIN_MAX_M = 24, 16
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 
 class ChainProblem(ctypes.Structure):
@@ -137,6 +140,18 @@ def lib():
     L.w4a8_host_buffer_device_pointer.argtypes = [p, c.POINTER(c.c_void_p)]
     L.w4a8_selftest_bounded_wait.restype = i32
     L.w4a8_selftest_bounded_wait.argtypes = [c.c_uint64, p, p]
+    L.w4a8_quantize_act_blocks.restype = i32
+    L.w4a8_quantize_act_blocks.argtypes = [p, i64, i64, i64, i32, p, i32, p, i64, i64, p, i64, p]
+    L.w4a8_linear_fp8_blocks.restype = i32
+    L.w4a8_linear_fp8_blocks.argtypes = [p, i64, p, i64, i64, p, i64, p, i64, i64, p, i64, i32, p]
+    L.w4a8_linear_fp8_experts.restype = i32
+    L.w4a8_linear_fp8_experts.argtypes = [p, i64, p, i64, i64, p, i64, p, i64, i64, p, i64, i64, p, i64, i32, p]
+    L.w4a8_route_experts_workspace_bytes.restype = sz
+    L.w4a8_route_experts_workspace_bytes.argtypes = [i64, i64]
+    L.w4a8_route_experts.restype = i32
+    L.w4a8_route_experts.argtypes = [p, i32, i64, i64, i64, i32, i32, p, i32, i32, i32, i32, c.c_float, p, p, p, p, p, sz, p]
+    L.w4a8_combine_experts.restype = i32
+    L.w4a8_combine_experts.argtypes = [p, i32, i64, i64, p, p, i64, i32, i64, p, i64, p, i64, i32, p]
     L.w4a8_query_device_status.restype = i32
     L.w4a8_query_device_status.argtypes = [c.POINTER(c.c_uint)]
     L.w4a8_launch_count.restype = c.c_uint64
@@ -494,6 +509,90 @@ def linear_w8a8(x8, s_x, w8, s_w, out_dtype=OUT_BF16, out=None):
                                 0 if s_w.numel() == 1 else 1, N, K, _ptr(out), out.stride(0), int(out_dtype),
                                 _ptr(ws), nb, _stream())
     _check("w4a8_linear_w8a8", rc)
+    return out
+
+
+def quantize_act_blocks(x, input_kind=CHAIN_INPUT_PLAIN, slots=None, rows=None, out=None):
+    """w4a8_quantize_act_blocks: x BF16 [M, K], or [M, 2K] (gate, up) for CHAIN_INPUT_SILU_MUL; slots int32 [M, top_k]: the rows of
+    the result that each token is written to (of `rows`, M * top_k by default).  Returns (x8 uint8 [rows, K], s_x float32
+    [rows, ceil(K / 128)]); without slots row m is token m."""
+    if out is None:
+        import torch
+        K = x.shape[1] // 2 if input_kind == CHAIN_INPUT_SILU_MUL else x.shape[1]
+        if rows is None:
+            rows = x.shape[0] if slots is None else slots.numel()
+        out = (torch.empty((rows, K), dtype=torch.uint8, device=x.device),
+               torch.empty((rows, (K + GROUP - 1) // GROUP), dtype=torch.float32, device=x.device))
+    x8, s_x = out
+    rc = (_host or _load_host()).quantize_act_blocks(x, int(input_kind), slots, x8, s_x)
+    if rc != OK:
+        _check("w4a8_quantize_act_blocks", rc)
+    return x8, s_x
+
+
+def linear_fp8_blocks(x8, s_x, w8, s_w, out_dtype=OUT_BF16, out=None):
+    """w4a8_linear_fp8_blocks: x8 [M, K] with s_x float32 [M, ceil(K / 128)], w8 [N, K] with s_w float32 [ceil(N / 128),
+    ceil(K / 128)] (E4M3, as uint8 or torch.float8_e4m3fn).  Returns Y [M, N]."""
+    if out is None:
+        import torch
+        out = torch.empty((x8.shape[0], w8.shape[0]), dtype=torch.float32 if out_dtype == OUT_FP32 else torch.bfloat16,
+                          device=x8.device)
+    rc = (_host or _load_host()).linear_fp8(x8, s_x, None, w8, s_w, out, int(out_dtype))
+    if rc != OK:
+        _check("w4a8_linear_fp8_blocks", rc)
+    return out
+
+
+def linear_fp8_experts(x8, s_x, offsets, w8, s_w, out_dtype=OUT_BF16, out=None):
+    """w4a8_linear_fp8_experts: rows offsets[e] to offsets[e + 1] (int32 [E + 1]) of x8 with the weights w8[e] of [E, N, K], s_w
+    float32 [E, ceil(N / 128), ceil(K / 128)].  Returns Y [rows, N]; rows of no expert are left as they were (undefined when
+    `out` is not given)."""
+    if out is None:
+        import torch
+        out = torch.empty((x8.shape[0], w8.shape[1]), dtype=torch.float32 if out_dtype == OUT_FP32 else torch.bfloat16,
+                          device=x8.device)
+    rc = (_host or _load_host()).linear_fp8(x8, s_x, offsets, w8, s_w, out, int(out_dtype))
+    if rc != OK:
+        _check("w4a8_linear_fp8_experts", rc)
+    return out
+
+
+def route_experts(logits, top_k, score=SCORE_SOFTMAX, bias=None, groups=1, top_groups=1, group_best=1, renormalize=True,
+                  scale=1.0, out=None, workspace=None):
+    """w4a8_route_experts: logits BF16 or FP32 [M, E].  Returns (ids int32 [M, top_k], weights float32 [M, top_k], offsets int32
+    [E + 1], slots int32 [M, top_k]).  `workspace`: any scratch tensor of w4a8_route_experts_workspace_bytes(M, E) bytes."""
+    host = _host or _load_host()
+    M, E = logits.shape
+    if out is None or workspace is None:
+        import torch
+        dev = logits.device
+        if out is None:
+            out = (torch.empty((M, top_k), dtype=torch.int32, device=dev), torch.empty((M, top_k), dtype=torch.float32, device=dev),
+                   torch.empty((E + 1,), dtype=torch.int32, device=dev), torch.empty((M, top_k), dtype=torch.int32, device=dev))
+        if workspace is None:
+            need = route_experts_workspace_bytes(M, E)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+    rc = host.route_experts(logits, int(score), bias, int(groups), int(top_groups), int(group_best), bool(renormalize), float(scale),
+                            *out, workspace)
+    if rc != OK:
+        _check("w4a8_route_experts", rc)
+    return out
+
+
+def route_experts_workspace_bytes(M, experts) -> int:
+    return int(lib().w4a8_route_experts_workspace_bytes(M, experts))
+
+
+def combine_experts(y, slots, weights, add=None, out_dtype=OUT_BF16, out=None):
+    """w4a8_combine_experts: y BF16 or FP32 [rows, N]; slots int32 and weights float32 [M, top_k]; add [M, N] of the result's type or
+    None.  Returns [M, N]."""
+    if out is None:
+        import torch
+        out = torch.empty((slots.shape[0], y.shape[1]), dtype=torch.float32 if out_dtype == OUT_FP32 else torch.bfloat16,
+                          device=y.device)
+    rc = (_host or _load_host()).combine_experts(y, slots, weights, add, out)
+    if rc != OK:
+        _check("w4a8_combine_experts", rc)
     return out
 
 

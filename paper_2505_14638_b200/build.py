@@ -4,19 +4,21 @@ calls (a small extension module against torch's headers) with the host compiler.
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libw4a8_b200.so")
 HOST_PATH = os.path.join(_HERE, "_w4a8_host.so")
-SOURCES = [os.path.join(CSRC, "w4a8_lib.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("w4a8_lib.cu", "w4a8_blocks_lib.cu")]
 HOST_SOURCE = os.path.join(CSRC, "w4a8_host.cpp")
 
 
 def _deps():
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))]
     deps.append(os.path.join(os.path.dirname(_HERE), "include", "w4a8.h"))
     return deps
 
@@ -32,6 +34,27 @@ def nvcc_command(out_path: str, verbose: bool = False):
     if verbose:
         cmd += ["-Xptxas", "-v"]
     return cmd + SOURCES + ["-lcudart"]
+
+
+def object_path(source: str) -> str:
+    return os.path.splitext(source)[0] + ".o"
+
+
+def object_deps(source: str):
+    """The source and what it includes from this repository."""
+    seen, todo = [], [source]
+    while todo:
+        path = os.path.normpath(todo.pop())
+        if path in seen or not os.path.exists(path):
+            continue
+        seen.append(path)
+        with open(path) as f:
+            todo += [os.path.join(os.path.dirname(path), name) for name in re.findall(r'^\s*#\s*include\s+"([^"]+)"', f.read(), re.M)]
+    return seen
+
+
+def object_command(source: str, out_path: str, verbose: bool = False):
+    return [a for a in nvcc_command(out_path, verbose) if a not in SOURCES + ["-shared", "-lcudart"]] + ["-c", source]
 
 
 def host_versions() -> str:
@@ -87,8 +110,17 @@ def _has_torch():
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """The C-ABI library alone."""
     if force or _stale(LIB_PATH, _deps()):
+        def compile_object(source):
+            out = object_path(source)
+            if force or _stale(out, object_deps(source)):
+                tmp = out + ".tmp%d.o" % os.getpid()
+                _run(object_command(source, tmp, verbose), out, tmp, "nvcc", verbose)
+            return out
+
+        with ThreadPoolExecutor(len(SOURCES)) as pool:   # (each waits for a compiler process)
+            objects = list(pool.map(compile_object, SOURCES))
         tmp = LIB_PATH + ".tmp%d" % os.getpid()
-        _run(nvcc_command(tmp, verbose), LIB_PATH, tmp, "nvcc", verbose)
+        _run([a for a in nvcc_command(tmp) if a not in SOURCES + ["-lcudart"]] + objects + ["-lcudart"], LIB_PATH, tmp, "nvcc")
     return LIB_PATH
 
 

@@ -1,0 +1,160 @@
+// Activations to E4M3 with one scale per token and block of 128 columns (plain or gated, optionally written to the rows that
+// the experts of each token read), and the weighted sum of the experts' outputs of each token.  Both are bound by HBM.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "w4a8_common.cuh"
+#include "w4a8_ptx.cuh"
+
+namespace w4a8 {
+
+// Maxima below this count as this one, so that 448 / maximum stays finite.
+constexpr float kBlockLeastMax = 7.888609052210118e-31f;   // 2^-100
+
+// Scale and its inverse of a block whose largest magnitude is `amax` (Eq. 13 per block).
+__device__ __forceinline__ void block_scale(float amax, float& s, float& inv) {
+    const float a = fmaxf(amax, kBlockLeastMax);
+    s = amax == 0.0f ? 1.0f : __fdiv_rn(a, kE4M3Max);
+    inv = amax == 0.0f ? 1.0f : __fdiv_rn(kE4M3Max, a);
+}
+
+// Eight lanes hold a block, 16 consecutive columns each; a warp takes four consecutive blocks of a row.  K % 16 == 0, so a lane
+// lies inside the row or outside.  The gated kind keeps silu(gate) * up in FP32: a rounding to BF16 in between would only add
+// an error.
+// top_k == 0: row m of the result is row m.  Otherwise it is written to the rows slots[m][0..top_k), entries outside [0, rows)
+// skipped: a token is read and quantized once however many experts read it.
+template <bool GATED>
+__global__ void __launch_bounds__(256)
+quantize_blocks_kernel(const uint16_t* __restrict__ x, int M, int K, int64_t ldx, const int32_t* __restrict__ slots, int top_k,
+                       uint8_t* __restrict__ x8, int64_t rows, int64_t ldx8, float* __restrict__ s_x, int64_t lds) {
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    const int lane = threadIdx.x & 31;
+    const int per_row = (K + 511) >> 9;   // warps' pieces of a row
+    const int64_t pieces = (int64_t)M * per_row;
+    const int64_t step = (int64_t)gridDim.x * (blockDim.x >> 5);
+    for (int64_t p = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); p < pieces; p += step) {
+        const int64_t m = p / per_row;
+        const int col = (int)(p - m * per_row) * 512 + lane * 16;
+        const bool have = col < K;
+        float v[16];
+        if (have) {
+            const uint4* src = reinterpret_cast<const uint4*>(x + m * ldx + col);
+            const uint4 a = __ldg(src), b = __ldg(src + 1);
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+            if constexpr (GATED) {
+                const uint4* up = reinterpret_cast<const uint4*>(x + m * ldx + K + col);
+                const uint4 c = __ldg(up), d = __ldg(up + 1);
+                const uint32_t u[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[2 * i] = __fdiv_rn(v[2 * i], 1.0f + expf(-v[2 * i])) * __uint_as_float(u[i] << 16);
+                    v[2 * i + 1] = __fdiv_rn(v[2 * i + 1], 1.0f + expf(-v[2 * i + 1])) * __uint_as_float(u[i] & 0xFFFF0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+        }
+        float amax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(v[i]));
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+        float s, inv;
+        block_scale(amax, s, inv);
+        uint4 q;
+        q.x = cvt_e4m3x4(__fmul_rn(v[0], inv), __fmul_rn(v[1], inv), __fmul_rn(v[2], inv), __fmul_rn(v[3], inv));
+        q.y = cvt_e4m3x4(__fmul_rn(v[4], inv), __fmul_rn(v[5], inv), __fmul_rn(v[6], inv), __fmul_rn(v[7], inv));
+        q.z = cvt_e4m3x4(__fmul_rn(v[8], inv), __fmul_rn(v[9], inv), __fmul_rn(v[10], inv), __fmul_rn(v[11], inv));
+        q.w = cvt_e4m3x4(__fmul_rn(v[12], inv), __fmul_rn(v[13], inv), __fmul_rn(v[14], inv), __fmul_rn(v[15], inv));
+        if (!have) continue;   // (no warp-wide step follows)
+        if (top_k == 0) {
+            *reinterpret_cast<uint4*>(x8 + m * ldx8 + col) = q;
+            if ((lane & 7) == 0) s_x[m * lds + (col >> 7)] = s;
+        } else {
+            for (int j = 0; j < top_k; ++j) {
+                const int64_t r = __ldg(slots + m * top_k + j);
+                if (r < 0 || r >= rows) continue;
+                *reinterpret_cast<uint4*>(x8 + r * ldx8 + col) = q;
+                if ((lane & 7) == 0) s_x[r * lds + (col >> 7)] = s;
+            }
+        }
+    }
+}
+
+// Eight consecutive values of a row as FP32.
+__device__ __forceinline__ void load8(const void* base, int64_t at, bool fp32, float (&v)[8]) {
+    if (fp32) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+        const float4 a = __ldg(p), b = __ldg(p + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t bf16x2_bits(float lo, float hi) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+// out[m] = add[m] + sum_j weights[m][j] * y[slots[m][j]]: FP32 sums in ascending order of j behind the added row, rounded once.
+// A thread holds eight columns of a token; the rows of four experts are in flight at a time.
+template <bool Y32, bool OUT32>
+__global__ void __launch_bounds__(256)
+combine_experts_kernel(const void* __restrict__ y, int64_t rows, int64_t ldy, const int32_t* __restrict__ slots,
+                       const float* __restrict__ weights, int64_t M, int top_k, int N, const void* __restrict__ add, int64_t ldadd,
+                       void* __restrict__ out, int64_t ldo) {
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    const int per_row = N >> 3;
+    const int64_t pieces = M * per_row, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; p < pieces; p += step) {
+        const int64_t m = p / per_row;
+        const int col = (int)(p - m * per_row) * 8;
+        float acc[8] = {};
+        if (add != nullptr) load8(add, m * ldadd + col, OUT32, acc);
+        for (int j0 = 0; j0 < top_k; j0 += 4) {
+            float v[4][8], w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t r = j0 + j < top_k ? (int64_t)__ldg(slots + m * top_k + j0 + j) : -1;
+                const bool have = r >= 0 && r < rows;
+                w[j] = have ? __ldg(weights + m * top_k + j0 + j) : 0.0f;
+                if (have) {
+                    load8(y, r * ldy + col, Y32, v[j]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
+        }
+        if constexpr (OUT32) {
+            float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + m * ldo + col);
+            o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        } else {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + m * ldo + col) =
+                make_uint4(bf16x2_bits(acc[0], acc[1]), bf16x2_bits(acc[2], acc[3]), bf16x2_bits(acc[4], acc[5]), bf16x2_bits(acc[6], acc[7]));
+        }
+    }
+}
+
+}  // namespace w4a8

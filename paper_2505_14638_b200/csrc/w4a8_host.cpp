@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -113,7 +114,180 @@ PyObject* linear_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- FP8 layers with block scales, mixture of experts -----------------------------------------------------------
+// Tensors may live on another device than the current one: the call runs there, on that device's current stream.
+const at::Tensor& on_device(PyObject* o, const char* what, at::ScalarType type, int64_t dim) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != dim || (dim > 0 && t.size(dim - 1) > 1 && t.stride(dim - 1) != 1)) {
+        PyErr_Format(PyExc_AssertionError, "%s: expected a %s tensor of %d dimensions on the device, contiguous along the last", what,
+                     c10::toString(type), static_cast<int>(dim));
+        throw Raised{};
+    }
+    return t;
+}
+const at::Tensor& e4m3(PyObject* o, const char* what, int64_t dim) {
+    return on_device(o, what, tensor(o).scalar_type() == at::kFloat8_e4m3fn ? at::kFloat8_e4m3fn : at::kByte, dim);
+}
+// W4A8_OUT_*; also checks what on_device checks
+int dtype_of(PyObject* o, const char* what, int64_t dim) {
+    const bool fp32 = tensor(o).scalar_type() == at::kFloat;
+    on_device(o, what, fp32 ? at::kFloat : at::kBFloat16, dim);
+    return fp32 ? W4A8_OUT_FP32 : W4A8_OUT_BF16;
+}
+void same_device(const at::Tensor& a, const at::Tensor& b) { check(a.device() == b.device(), "tensors on different devices"); }
+
+template <class F>
+int run_on(const at::Tensor& t, F f) {
+    const c10::cuda::CUDAGuard guard(t.device());
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f(stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+int64_t blocks_of(int64_t n) { return (n + 127) / 128; }
+
+// (x, input_kind, slots or None, x8, s_x) -> status
+PyObject* quantize_act_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() -> int {
+        const at::Tensor &x = on_device(a[0], "x", at::kBFloat16, 2), &x8 = e4m3(a[3], "x8", 2), &s_x = on_device(a[4], "s_x", at::kFloat, 2);
+        const int kind = static_cast<int>(integer(a[1]));
+        const int64_t K = kind == W4A8_CHAIN_INPUT_SILU_MUL ? x.size(1) / 2 : x.size(1);
+        check(kind != W4A8_CHAIN_INPUT_SILU_MUL || x.size(1) % 2 == 0, "x: gate and up of equal width");
+        check(x8.size(1) == K && s_x.size(1) == blocks_of(K) && s_x.size(0) == x8.size(0), "x8 [rows, K] and s_x [rows, ceil(K / 128)]");
+        same_device(x, x8);
+        same_device(x, s_x);
+        const int32_t* slots = nullptr;
+        int top_k = 0;
+        if (a[2] != Py_None) {
+            const at::Tensor& t = on_device(a[2], "slots", at::kInt, 2);
+            check(t.is_contiguous() && t.size(0) == x.size(0), "slots: [M, top_k], contiguous");
+            same_device(x, t);
+            slots = static_cast<const int32_t*>(t.data_ptr());
+            top_k = static_cast<int>(t.size(1));
+        }
+        return run_on(x, [&](void* stream) {
+            return w4a8_quantize_act_blocks(x.data_ptr(), x.size(0), K, x.stride(0), kind, slots, top_k, static_cast<uint8_t*>(x8.data_ptr()),
+                                            x8.size(0), x8.stride(0), static_cast<float*>(s_x.data_ptr()), s_x.stride(0), stream);
+        });
+    });
+}
+
+// (x8, s_x, offsets or None, w8, s_w, out, out_dtype) -> status; with offsets the experts' products
+PyObject* linear_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> int {
+        const bool experts = a[2] != Py_None;
+        const int64_t d = experts ? 3 : 2;
+        const at::Tensor &x8 = e4m3(a[0], "x8", 2), &s_x = on_device(a[1], "s_x", at::kFloat, 2), &w8 = e4m3(a[3], "w8", d),
+                         &s_w = on_device(a[4], "s_w", at::kFloat, d), &out = tensor(a[5]);
+        const int od = static_cast<int>(integer(a[6]));
+        check(dtype_of(a[5], "out", 2) == od, "out and out_dtype differ");
+        const int64_t M = x8.size(0), K = x8.size(1), N = w8.size(d - 2), E = experts ? w8.size(0) : 1;
+        check(w8.size(d - 1) == K, "x8 and w8 differ in K");
+        check(s_x.size(0) == M && s_x.size(1) == blocks_of(K), "s_x: [M, ceil(K / 128)]");
+        check(s_w.is_contiguous() && s_w.size(d - 2) == blocks_of(N) && s_w.size(d - 1) == blocks_of(K) && (!experts || s_w.size(0) == E),
+              "s_w: a scale per 128 x 128 weights, contiguous");
+        check(out.size(0) == M && out.size(1) == N, "out: [M, N]");
+        same_device(x8, s_x);
+        same_device(x8, w8);
+        same_device(x8, s_w);
+        same_device(x8, out);
+        const uint8_t *xp = static_cast<const uint8_t*>(x8.data_ptr()), *wp = static_cast<const uint8_t*>(w8.data_ptr());
+        const float *sx = static_cast<const float*>(s_x.data_ptr()), *sw = static_cast<const float*>(s_w.data_ptr());
+        if (!experts)
+            return run_on(x8, [&](void* stream) {
+                return w4a8_linear_fp8_blocks(xp, x8.stride(0), sx, s_x.stride(0), M, wp, w8.stride(0), sw, N, K, out.data_ptr(),
+                                              out.stride(0), od, stream);
+            });
+        const at::Tensor& offsets = on_device(a[2], "offsets", at::kInt, 1);
+        check(offsets.size(0) == E + 1, "offsets: [experts + 1]");
+        same_device(x8, offsets);
+        return run_on(x8, [&](void* stream) {
+            return w4a8_linear_fp8_experts(xp, x8.stride(0), sx, s_x.stride(0), M, static_cast<const int32_t*>(offsets.data_ptr()), E, wp,
+                                           w8.stride(1), w8.stride(0), sw, N, K, out.data_ptr(), out.stride(0), od, stream);
+        });
+    });
+}
+
+// (logits, score, bias or None, groups, top_groups, group_best, renormalize, scale, ids, weights, offsets, slots, workspace or None) -> status
+PyObject* route_experts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> int {
+        const int dtype = dtype_of(a[0], "logits", 2);
+        const at::Tensor &logits = tensor(a[0]), &ids = on_device(a[8], "ids", at::kInt, 2), &weights = on_device(a[9], "weights", at::kFloat, 2),
+                         &offsets = on_device(a[10], "offsets", at::kInt, 1), &slots = on_device(a[11], "slots", at::kInt, 2);
+        const int64_t M = logits.size(0), E = logits.size(1), k = ids.size(1);
+        check(ids.is_contiguous() && weights.is_contiguous() && slots.is_contiguous() && ids.size(0) == M && weights.sizes() == ids.sizes() &&
+                  slots.sizes() == ids.sizes() && offsets.size(0) == E + 1,
+              "ids, weights and slots: [M, top_k], contiguous; offsets: [E + 1]");
+        const float* bias = nullptr;
+        if (a[2] != Py_None) {
+            const at::Tensor& b = on_device(a[2], "bias", at::kFloat, 1);
+            check(b.size(0) == E, "bias: [E]");
+            same_device(logits, b);
+            bias = static_cast<const float*>(b.data_ptr());
+        }
+        void* ws = nullptr;
+        size_t wsn = 0;
+        if (a[12] != Py_None) {
+            const at::Tensor& w = tensor(a[12]);
+            check(w.is_cuda() && w.is_contiguous(), "workspace: contiguous, on the device");
+            same_device(logits, w);
+            ws = w.data_ptr();
+            wsn = w.nbytes();
+        }
+        same_device(logits, ids);
+        same_device(logits, weights);
+        same_device(logits, offsets);
+        same_device(logits, slots);
+        const int score = static_cast<int>(integer(a[1])), groups = static_cast<int>(integer(a[3])), top_groups = static_cast<int>(integer(a[4])),
+                  best = static_cast<int>(integer(a[5])), renormalize = static_cast<int>(integer(a[6]));
+        const double scale = PyFloat_AsDouble(a[7]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
+        return run_on(logits, [&](void* stream) {
+            return w4a8_route_experts(logits.data_ptr(), dtype, M, logits.stride(0), E, static_cast<int>(k), score, bias, groups, top_groups, best,
+                                      renormalize, static_cast<float>(scale), static_cast<int32_t*>(ids.data_ptr()),
+                                      static_cast<float*>(weights.data_ptr()), static_cast<int32_t*>(offsets.data_ptr()),
+                                      static_cast<int32_t*>(slots.data_ptr()), ws, wsn, stream);
+        });
+    });
+}
+
+// (y, slots, weights, add or None, out) -> status
+PyObject* combine_experts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() -> int {
+        const int yd = dtype_of(a[0], "y", 2), od = dtype_of(a[4], "out", 2);
+        const at::Tensor &y = tensor(a[0]), &out = tensor(a[4]), &slots = on_device(a[1], "slots", at::kInt, 2),
+                         &weights = on_device(a[2], "weights", at::kFloat, 2);
+        const int64_t M = slots.size(0), N = y.size(1);
+        check(slots.is_contiguous() && weights.is_contiguous() && weights.sizes() == slots.sizes(), "slots and weights: [M, top_k], contiguous");
+        check(out.size(0) == M && out.size(1) == N, "out: [M, N]");
+        const void* add = nullptr;
+        int64_t ldadd = 0;
+        if (a[3] != Py_None) {
+            const at::Tensor& t = tensor(a[3]);
+            check(dtype_of(a[3], "add", 2) == od && t.sizes() == out.sizes(), "add: of the shape and type of the result");
+            same_device(y, t);
+            add = t.data_ptr();
+            ldadd = t.stride(0);
+        }
+        same_device(y, slots);
+        same_device(y, weights);
+        same_device(y, out);
+        return run_on(y, [&](void* stream) {
+            return w4a8_combine_experts(y.data_ptr(), yd, y.size(0), y.stride(0), static_cast<const int32_t*>(slots.data_ptr()),
+                                        static_cast<const float*>(weights.data_ptr()), M, static_cast<int>(slots.size(1)), N, add, ldadd,
+                                        out.data_ptr(), out.stride(0), od, stream);
+        });
+    });
+}
+
 PyMethodDef methods[] = {
+    {"quantize_act_blocks", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize_act_blocks)), METH_FASTCALL, nullptr},
+    {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_fp8)), METH_FASTCALL, nullptr},
+    {"route_experts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(route_experts)), METH_FASTCALL, nullptr},
+    {"combine_experts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(combine_experts)), METH_FASTCALL, nullptr},
     {"quantize_act", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize_act)), METH_FASTCALL, nullptr},
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear)), METH_FASTCALL, nullptr},
     {"linear_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_workspace_bytes)), METH_FASTCALL, nullptr},

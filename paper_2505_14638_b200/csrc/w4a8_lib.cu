@@ -11,6 +11,7 @@
 #include "../../include/w4a8.h"
 #include "w4a8_decode_plan.h"
 #include "w4a8_dpq_kernels.cuh"
+#include "w4a8_internal.h"
 #include "w4a8_linear_chain.cuh"
 #include "w4a8_linear_direct.cuh"
 #include "w4a8_linear_rows.cuh"
@@ -26,9 +27,9 @@ __device__ unsigned int g_status_word = 0;  // bit mask, see kStatus*
 
 static std::atomic<uint64_t> g_launches{0};
 
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
-static int check_device() {
+int check_device() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return W4A8_ERR_CUDA;
     static std::mutex mu;
@@ -44,7 +45,7 @@ static int check_device() {
     return cached_major == 10 ? W4A8_OK : W4A8_ERR_UNSUPPORTED_DEVICE;
 }
 
-static unsigned int* status_word_ptr() {
+unsigned int* status_word_ptr() {
     // Address of the device status word on the current device (looked up once per device).
     static std::mutex mu;
     static unsigned int* ptrs[64] = {nullptr};
@@ -92,17 +93,12 @@ static void* static_scratch_ptr() {
     return ptrs[dev];
 }
 
-static inline int launch_status() {
+int launch_status() {
     return cudaGetLastError() == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
 }
 
 // ------------------------------------------------------------------------------ tensor maps
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn() {
+EncodeTiledFn encode_tiled_fn() {
     static EncodeTiledFn fn = nullptr;
     static std::once_flag once;
     std::call_once(once, [] {
@@ -219,7 +215,7 @@ static int launch_umma(const CUtensorMap& tw, const CUtensorMap& tx, const uint1
 }
 
 // ------------------------------------------------------------------------------ persistent kernel plan
-static int sm_count() {
+int sm_count() {
     static std::mutex mu;
     static int cached_dev = -1, cached = 0;
     int dev = 0;

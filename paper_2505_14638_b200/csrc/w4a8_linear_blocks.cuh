@@ -1,0 +1,388 @@
+// FP8 linear layers with a scale per block of 128 (activations: one per token and 128 columns; weights: one per 128 x 128):
+//   y[m][n] = sum_b s_x[m][b] * s_w[n / 128][b] * P_b[m][n],   P_b[m][n] = sum over the 128 columns of block b of x8 * w8,
+// of one layer, or of several experts whose rows lie one behind the other.
+//
+// linear_blocks_kernel: a tile is 128 output channels x up to TMAX tokens.  P_b is one k-block's MMAs into a buffer of its own in
+// tensor memory (FP32); four warps, a thread per channel, fetch it and add s_x * s_w times it to sums in registers -- the scales
+// change with every k-block, so the tensor cores cannot go on adding.  The weights are the A operand (128 rows), the tokens the
+// B operand (N = the tile's tokens rounded up to 16), so that few tokens cost few columns.
+//
+// Few tokens are bound by the weight stream: one stage of the ring is a k-block of weights (16 KB) with its activations, loaded by
+// TMA in the 128-byte swizzle.  Where the tiles do not fill the SMs, the CTAs of a cluster take a part of K each and exchange
+// their sums through distributed shared memory: each adds the parts of its share of the channels, in ascending order of K, so
+// results repeat.  No workspace is needed, so nothing of one call can meet another's.
+//
+// Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 idle after the start, 4..7 sums and outputs.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "w4a8_common.cuh"
+#include "w4a8_ptx.cuh"
+
+namespace w4a8 {
+
+constexpr int kBlocksMaxExperts = 512;
+constexpr int kBlocksThreads = 256;
+constexpr int kBlocksMaxStages = 16, kBlocksBuffers = 4;
+constexpr int kBlocksChunk = 8;    // k-blocks whose activation scales are fetched at a time
+
+struct BlocksParams {
+    const float *s_x, *s_w;
+    const int32_t* offsets;   // [E + 1]; NULL: one layer, all rows
+    void* y;
+    int64_t lds, ldy, rows;
+    int E, N, KB, NB;         // experts; channels; k-blocks; channel blocks
+    int cut;                  // CTAs (a cluster) that share a tile's K
+    int stages, xslot;        // ring: stages, bytes of a stage's activations (whole boxes of 32 tokens)
+    int tokens;               // tokens of a tile at most
+    int out_fp32;
+    unsigned int* status;
+};
+
+// Where the experts' rows and token tiles begin, in shared memory.
+struct ExpertTable {
+    int32_t row[kBlocksMaxExperts + 1];    // first row; row[E] = end of the last
+    int32_t tile[kBlocksMaxExperts + 1];   // token tiles of the experts before
+};
+
+// The first warp fills the table.  Offsets are taken into [0, rows] and in ascending order, whatever they hold.
+__device__ __forceinline__ void fill_expert_table(ExpertTable* t, const int32_t* offsets, int E, int64_t rows, int tokens) {
+    const int lane = threadIdx.x & 31;
+    const int32_t most = (int32_t)rows;
+    int32_t begin_all = 0, tiles = 0;
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+        const int e = e0 + lane;
+        int32_t r = e <= E ? min(max(__ldg(offsets + e), 0), most) : most;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t before = __shfl_up_sync(0xFFFFFFFFu, r, o);
+            if (lane >= o) r = max(r, before);
+        }
+        r = max(r, begin_all);
+        begin_all = __shfl_sync(0xFFFFFFFFu, r, 31);
+        if (e <= E) t->row[e] = r;
+    }
+    __syncwarp();
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane;
+        const int32_t own = e < E ? (t->row[e + 1] - t->row[e] + tokens - 1) / tokens : 0;
+        int32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t before = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= o) sum += before;
+        }
+        if (e < E) t->tile[e] = tiles + sum - own;
+        tiles += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    if (lane == 0) t->tile[E] = tiles;
+}
+
+// Tile index -> expert, channel block and rows.  The channel blocks of a token tile follow one another.
+struct BlocksTile {
+    int e, nb, count;   // expert, channel block, tokens
+    int64_t row;        // first row
+};
+__device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const ExpertTable* t, int i) {
+    BlocksTile b;
+    const int j = i / p.NB;
+    b.nb = i - j * p.NB;
+    if (p.offsets == nullptr) {
+        b.e = 0;
+        b.row = (int64_t)j * p.tokens;
+        b.count = (int)min((int64_t)p.tokens, p.rows - b.row);
+        return b;
+    }
+    int lo = 0, hi = p.E;   // the last expert whose tiles begin at or before j
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t->tile[mid] <= j) lo = mid; else hi = mid;
+    }
+    b.e = lo;
+    const int at = (j - t->tile[lo]) * p.tokens;
+    b.row = t->row[lo] + at;
+    b.count = min(p.tokens, t->row[lo + 1] - t->row[lo] - at);
+    return b;
+}
+
+// Arrival on a barrier of a CTA of the cluster that also announces this thread's writes to that CTA's shared memory, and the wait
+// that goes with it.
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+template <int TMAX_>
+struct BlocksCfg {
+    static constexpr int TMAX = TMAX_;
+    static constexpr int kAccCols = TMAX_ < 32 ? 32 : TMAX_;
+    static constexpr int kTmemCols = kBlocksBuffers * kAccCols;
+    static constexpr int kBarBytes = 8 * (2 * kBlocksMaxStages + 2 * kBlocksBuffers + 2 + 1) + 16;
+    // (behind the ring) barriers, scales [2][chunk][TMAX], experts, parts of other CTAs [cut][TMAX][channels of a share]
+    static constexpr int kScaleBytes = 2 * kBlocksChunk * TMAX_ * 4;
+    __host__ __device__ static constexpr int table_bytes(bool grouped) { return grouped ? (int)sizeof(ExpertTable) : 0; }
+    __host__ __device__ static constexpr int part_bytes(int cut) { return cut > 1 ? cut * ((128 + cut - 1) / cut) * TMAX_ * 4 : 0; }
+    static constexpr int kSmemMax = 232448;
+    __host__ __device__ static constexpr int fixed_bytes(bool grouped, int cut) {
+        return 1024 + ((kBarBytes + 15) / 16 * 16) + kScaleBytes + (table_bytes(grouped) + 15) / 16 * 16 + part_bytes(cut);
+    }
+};
+
+template <class Cfg>
+__global__ void __launch_bounds__(kBlocksThreads, 1)
+linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
+                     const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 32, 128B swizzle
+                     const BlocksParams p) {
+    constexpr int TMAX = Cfg::TMAX, NBUF = kBlocksBuffers;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = ptx::smem_addr(smem_raw);
+    const uint32_t base = (raw_addr + 1023u) & ~1023u;
+    uint8_t* sm = smem_raw + (base - raw_addr);
+    const uint32_t stage_bytes = 16384u + (uint32_t)p.xslot;
+    uint32_t off = (uint32_t)p.stages * stage_bytes;
+    const uint32_t bars = base + off;
+    const uint32_t bar_full = bars, bar_free = bar_full + 8u * kBlocksMaxStages;
+    const uint32_t bar_acc = bar_free + 8u * kBlocksMaxStages, bar_acc_free = bar_acc + 8u * NBUF;
+    const uint32_t bar_parts = bar_acc_free + 8u * NBUF, bar_parts_free = bar_parts + 8u, bar_drain = bar_parts + 16u;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + off + 8u * (2 * kBlocksMaxStages + 2 * NBUF + 3));
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    off += (uint32_t)(Cfg::kBarBytes + 15) / 16u * 16u;
+    float* scales = reinterpret_cast<float*>(sm + off);   // [2][chunk][TMAX]
+    off += (uint32_t)Cfg::kScaleBytes;
+    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + off);
+    off += (uint32_t)(Cfg::table_bytes(p.offsets != nullptr) + 15) / 16u * 16u;
+    float* parts = reinterpret_cast<float*>(sm + off);    // [cut][TMAX][share]
+    const uint32_t parts_addr = base + off;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cut = p.cut, rank = cut > 1 ? (int)ptx::cluster_ctarank() : 0;
+    const int share = (128 + cut - 1) / cut;
+    const int kb0 = rank * p.KB / cut, KB = (rank + 1) * p.KB / cut - kb0;
+
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), Cfg::kTmemCols);
+        ptx::tmem_relinquish();
+    } else if (warp == 2) {
+        if (lane == 0) {
+            for (int i = 0; i < p.stages; ++i) {
+                ptx::mbar_init(bar_full + 8u * i, 1);
+                ptx::mbar_init(bar_free + 8u * i, 1);
+            }
+            for (int i = 0; i < NBUF; ++i) {
+                ptx::mbar_init(bar_acc + 8u * i, 1);
+                ptx::mbar_init(bar_acc_free + 8u * i, 4);
+            }
+            ptx::mbar_init(bar_parts, (uint32_t)cut * 4u);
+            ptx::mbar_init(bar_parts_free, (uint32_t)cut);
+            ptx::mbar_init(bar_drain, 1);
+            *abort_flag = 0u;
+            ptx::fence_mbar_init();
+        }
+    } else if (warp == 3 && lane == 0) {
+        ptx::prefetch_tensormap(&tmap_w);
+        ptx::prefetch_tensormap(&tmap_x);
+    }
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    if (warp == 0 && p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (cut > 1) ptx::cluster_sync_all();   // (barriers of the peers are there before anything arrives on them)
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    const int token_tiles = p.offsets != nullptr ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
+    const int tiles = token_tiles * p.NB;
+    const int first = (int)blockIdx.x / cut, step = (int)gridDim.x / cut;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ loads (whole warp, one lane issues)
+        bool ok = true;
+        ptx::Ring r;
+        int issued = 0;
+        for (int i = first; i < tiles && ok; i += step) {
+            const BlocksTile t = blocks_tile(p, table, i);
+            const int boxes = (t.count + 31) >> 5;
+            const uint32_t bytes = 16384u + (uint32_t)boxes * 4096u;
+            for (int b = 0; b < KB; ++b) {
+                if (issued >= p.stages) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                const uint32_t full = bar_full + 8u * r.idx, dst = base + (uint32_t)r.idx * stage_bytes;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(full, bytes);
+                    ptx::tma_load_3d(dst, &tmap_w, (kb0 + b) * 128, t.nb * 128, t.e, full);
+                    for (int q = 0; q < boxes; ++q)
+                        ptx::tma_load_2d(dst + 16384u + (uint32_t)q * 4096u, &tmap_x, (kb0 + b) * 128, (int)t.row + 32 * q, full);
+                }
+                r.advance(p.stages);
+                ++issued;
+            }
+        }
+        if (!ok && lane == 0) {   // gave up: let the copies in flight land before the CTA goes away
+            const uint64_t t0 = ptx::globaltimer_ns();
+            for (int i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i)
+                while (!ptx::mbar_try_wait(bar_full + 8u * (i % p.stages), (uint32_t)((i / p.stages) & 1)) &&
+                       ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 20) {
+                }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMAs (whole warp, one lane issues)
+        bool ok = true;
+        ptx::Ring r, a;
+        int made = 0;
+        for (int i = first; i < tiles && ok; i += step) {
+            const BlocksTile t = blocks_tile(p, table, i);
+            const uint32_t idesc = ptx::umma_idesc_e4m3_f32(128, 0) | (uint32_t)(((t.count + 15) & ~15) >> 3) << 17;
+            for (int b = 0; b < KB; ++b) {
+                if (made >= NBUF) ok = ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
+                ok = ok && ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t w = base + (uint32_t)r.idx * stage_bytes;
+                const uint32_t a_lo = ptx::umma_desc_lo(w), b_lo = ptx::umma_desc_lo(w + 16384u);
+                if (ptx::elect_one()) {
+                    ptx::umma_f8_kblock(tmem + (uint32_t)(a.idx * Cfg::kAccCols), a_lo, b_lo, idesc, 0u);
+                    ptx::umma_commit(bar_free + 8u * r.idx);
+                    ptx::umma_commit(bar_acc + 8u * a.idx);
+                }
+                r.advance(p.stages);
+                a.advance(NBUF);
+                ++made;
+            }
+        }
+        if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
+            ptx::umma_commit(bar_drain);
+            const uint64_t t0 = ptx::globaltimer_ns();
+            while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ sums and outputs: thread = channel of the tile
+        const int tid = (int)threadIdx.x - 128;   // channel within the tile; token in the scale fetches
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        bool ok = true;
+        ptx::Ring a;
+        uint32_t exchanged = 0;
+        int c = 0;
+        // (after a wait that gave up these warps still walk all tiles, without waiting or writing: they meet at a barrier)
+        for (int i = first; i < tiles; i += step) {
+            const BlocksTile t = blocks_tile(p, table, i);
+            const float* sw_row = p.s_w + ((int64_t)t.e * p.NB + t.nb) * p.KB + kb0;
+            const float* sx_row = p.s_x + (t.row + tid) * p.lds + kb0;
+            const bool token = tid < t.count;
+            unsigned long long acc[TMAX / 2];
+#pragma unroll
+            for (int j = 0; j < TMAX / 2; ++j) acc[j] = 0ull;
+            float next[kBlocksChunk];   // this thread's token's scales of the next chunk of k-blocks
+#pragma unroll
+            for (int j = 0; j < kBlocksChunk; ++j) next[j] = token && j < KB ? __ldg(sx_row + j) * __ldg(sw_row + j) : 0.0f;
+            for (int b0 = 0; b0 < KB; b0 += kBlocksChunk, c ^= 1) {
+                float* cur = scales + c * kBlocksChunk * TMAX;
+                if (tid < TMAX) {
+#pragma unroll
+                    for (int j = 0; j < kBlocksChunk; ++j) cur[j * TMAX + tid] = next[j];
+                }
+                // (two buffers: a warp writes a chunk's scales only when all have finished with the chunk before the last)
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < kBlocksChunk; ++j) {
+                    const int b = b0 + kBlocksChunk + j;
+                    next[j] = token && b < KB ? __ldg(sx_row + b) * __ldg(sw_row + b) : 0.0f;
+                }
+                const int end = min(kBlocksChunk, KB - b0);
+                for (int j = 0; j < end; ++j) {
+                    ok = ok && ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
+                    if (!ok) break;   // (warp-uniform)
+                    ptx::tc_fence_after_sync();
+                    const ulonglong2* f = reinterpret_cast<const ulonglong2*>(cur + j * TMAX);
+                    const uint32_t src = lanes + (uint32_t)(a.idx * Cfg::kAccCols);
+#pragma unroll
+                    for (int q = 0; q < TMAX / 16; ++q) {
+                        if (q * 16 >= t.count) break;
+                        uint32_t v[16];
+                        ptx::tmem_ld_32x32b_x16(src + (uint32_t)(q * 16), v);
+                        ptx::tmem_ld_wait_for(v);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const ulonglong2 s = f[q * 4 + h];   // the scales of four tokens
+                            acc[q * 8 + 2 * h] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h]), __uint_as_float(v[4 * h + 1])), s.x, acc[q * 8 + 2 * h]);
+                            acc[q * 8 + 2 * h + 1] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h + 2]), __uint_as_float(v[4 * h + 3])), s.y, acc[q * 8 + 2 * h + 1]);
+                        }
+                    }
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar_acc_free + 8u * a.idx);
+                    a.advance(NBUF);
+                }
+            }
+            if (cut == 1) {
+                const int n = t.nb * 128 + tid;
+                if (ok && n < p.N) {
+#pragma unroll
+                    for (int j = 0; j < TMAX / 2; ++j) {
+                        float lo, hi;
+                        unpack_f32x2(acc[j], lo, hi);
+                        const int64_t at = (t.row + 2 * j) * p.ldy + n;
+                        if (p.out_fp32) {
+                            if (2 * j < t.count) static_cast<float*>(p.y)[at] = lo;
+                            if (2 * j + 1 < t.count) static_cast<float*>(p.y)[at + p.ldy] = hi;
+                        } else {
+                            if (2 * j < t.count) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(lo);
+                            if (2 * j + 1 < t.count) static_cast<__nv_bfloat16*>(p.y)[at + p.ldy] = __float2bfloat16_rn(hi);
+                        }
+                    }
+                }
+                continue;
+            }
+            // The parts of this thread's channel go to the CTA that adds them, once that has read those of the tile before.
+            if (exchanged > 0) ok = ok && ptx::mbar_wait_warp(bar_parts_free, (exchanged - 1u) & 1u, abort_flag, p.status);
+            if (ok) {
+                const int owner = tid / share;
+                const uint32_t to = ptx::map_to_cta(parts_addr, (uint32_t)owner) + (uint32_t)((rank * TMAX * share + tid - owner * share) * 4);
+#pragma unroll
+                for (int j = 0; j < TMAX / 2; ++j) {
+                    float lo, hi;
+                    unpack_f32x2(acc[j], lo, hi);
+                    if (2 * j < t.count) st_cluster_f32(to + (uint32_t)(2 * j * share * 4), lo);
+                    if (2 * j + 1 < t.count) st_cluster_f32(to + (uint32_t)((2 * j + 1) * share * 4), hi);
+                }
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");
+                __syncwarp();
+                if (lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts, (uint32_t)lane));
+                ok = ptx::mbar_wait_warp(bar_parts, exchanged & 1u, abort_flag, p.status);
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");
+            }
+            if (ok) {
+                const int n0 = t.nb * 128 + rank * share, have = min(share, 128 - rank * share);
+                for (int e = tid; e < t.count * share; e += 128) {
+                    const int tok = e / share, c = e - tok * share;
+                    if (c >= have || n0 + c >= p.N) continue;
+                    float s = 0.0f;
+                    for (int q = 0; q < cut; ++q) s += parts[(q * TMAX + tok) * share + c];
+                    const int64_t at = (t.row + tok) * p.ldy + n0 + c;
+                    if (p.out_fp32)
+                        static_cast<float*>(p.y)[at] = s;
+                    else
+                        static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(s);
+                }
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (warp == 4 && lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts_free, (uint32_t)lane));
+            ++exchanged;
+        }
+    }
+
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, Cfg::kTmemCols);
+    }
+    if (cut > 1) ptx::cluster_sync_all();   // (no CTA goes away while another writes to its shared memory or arrives on its barriers)
+}
+
+}  // namespace w4a8
