@@ -135,7 +135,7 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     }
     {
         const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ldx8};
-        const cuuint32_t box[2] = {128, 32};
+        const cuuint32_t box[2] = {128, pl.pair ? 128u : 32u};
         if (!make_map(&tx, x8, 2, dims, strides, box)) return W4A8_ERR_CUDA;
     }
     BlocksParams p = {};
@@ -154,6 +154,12 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     p.tokens = pl.tokens;
     p.out_fp32 = out_dtype == W4A8_OUT_FP32 ? 1 : 0;
     p.status = status;
+    if (pl.pair) {
+        static std::atomic<uint64_t> allowed{0};
+        if (!allow_smem(linear_blocks_pair_kernel, allowed)) return W4A8_ERR_CUDA;
+        const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
+        return launch(linear_blocks_pair_kernel, (unsigned)(2 * pairs), kPairBlocksThreads, (size_t)pair_blocks_smem(offsets != nullptr), 2, st, tw, tx, p);
+    }
     switch (pl.tmax) {
         case 16: return launch_blocks<16>(tw, tx, p, sms, tiles, st);
         case 32: return launch_blocks<32>(tw, tx, p, sms, tiles, st);

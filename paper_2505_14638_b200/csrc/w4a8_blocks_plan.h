@@ -8,6 +8,7 @@ namespace w4a8 {
 constexpr int kBlocksSmemMax = 232448;
 
 struct BlocksPlan {
+    bool pair;     // CTA pairs: tiles of 256 tokens x 256 channels
     int tmax;      // tokens that the kernel's registers are laid out for: 16, 32, 64, 128
     int tokens;    // tokens of a tile at most
     int cut;       // CTAs that share a tile's K
@@ -24,6 +25,13 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
     if (experts > 1) {
         load = 4 * ceil_div(rows, experts) + 12;
         if (load > rows) load = rows;
+    }
+    pl.pair = rows > 128 * experts;
+    if (pl.pair) {
+        pl.tmax = 0;
+        pl.tokens = 256;
+        pl.cut = 1;
+        return pl;
     }
     pl.tmax = load <= 16 ? 16 : load <= 32 ? 32 : load <= 64 ? 64 : 128;
     pl.tokens = load >= 128 ? 128 : (int)ceil_div(load, 16) * 16;

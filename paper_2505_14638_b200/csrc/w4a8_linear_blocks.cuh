@@ -79,15 +79,15 @@ __device__ __forceinline__ void fill_expert_table(ExpertTable* t, const int32_t*
     if (lane == 0) t->tile[E] = tiles;
 }
 
-// Tile index -> expert, channel block and rows.  The channel blocks of a token tile follow one another.
+// A tile: expert, first channel block, rows.
 struct BlocksTile {
     int e, nb, count;   // expert, channel block, tokens
     int64_t row;        // first row
 };
-__device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const ExpertTable* t, int i) {
+// The rows of token tile j.
+__device__ __forceinline__ BlocksTile blocks_rows(const BlocksParams& p, const ExpertTable* t, int j) {
     BlocksTile b;
-    const int j = i / p.NB;
-    b.nb = i - j * p.NB;
+    b.nb = 0;
     if (p.offsets == nullptr) {
         b.e = 0;
         b.row = (int64_t)j * p.tokens;
@@ -103,6 +103,13 @@ __device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const E
     const int at = (j - t->tile[lo]) * p.tokens;
     b.row = t->row[lo] + at;
     b.count = min(p.tokens, t->row[lo + 1] - t->row[lo] - at);
+    return b;
+}
+// The channel blocks of a token tile follow one another.
+__device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const ExpertTable* t, int i) {
+    const int j = i / p.NB;
+    BlocksTile b = blocks_rows(p, t, j);
+    b.nb = i - j * p.NB;
     return b;
 }
 
@@ -383,6 +390,251 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
         ptx::tmem_dealloc(tmem, Cfg::kTmemCols);
     }
     if (cut > 1) ptx::cluster_sync_all();   // (no CTA goes away while another writes to its shared memory or arrives on its barriers)
+}
+
+// ---- many tokens: CTA pairs ----------------------------------------------------------------------------------------------------
+// Bound by the tensor cores.  A tile is 256 tokens x 256 channels of a CTA pair (cta_group::2): the tokens are the A operand, so that
+// a thread of the warps that add has one token and needs one product s_x * s_w per k-block and 128 channels; each CTA holds 128
+// tokens and the sums of all 256 channels: 128 registers in each of 256 threads.  Its k-block's MMAs (512 cycles) go into one of two
+// buffers of tensor memory while the other is fetched (256 columns: 256 cycles) and added.
+//
+// Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs.
+constexpr int kPairBlocksThreads = 320, kPairBlocksStages = 6;
+constexpr int kPairBlocksStageBytes = 32768;   // 128 tokens, 128 channels
+constexpr int kPairBlocksBand = 32;            // token tiles (8192 tokens) that share the channels' weights while they are in L2
+constexpr int kPairBlocksBars = 2 * kPairBlocksStages + 4 + 1;
+__host__ __device__ constexpr int pair_blocks_smem(bool grouped) {
+    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + 8 * kPairBlocksBars + 16 + (grouped ? (int)sizeof(ExpertTable) : 0);
+}
+
+// Tile index -> expert, pair of channel blocks and rows.
+__device__ __forceinline__ BlocksTile pair_blocks_tile(const BlocksParams& p, const ExpertTable* t, int i, int token_tiles) {
+    const int NT = (p.NB + 1) >> 1;
+    BlocksTile b;
+    if (p.offsets != nullptr) {
+        const int j = i / NT;
+        b = blocks_rows(p, t, j);
+        b.nb = 2 * (i - j * NT);
+        return b;
+    }
+    const int per = kPairBlocksBand * NT, band = i / per, in = i - band * per;
+    const int high = min(kPairBlocksBand, token_tiles - band * kPairBlocksBand), n = in / high;
+    b = blocks_rows(p, t, band * kPairBlocksBand + in - n * high);
+    b.nb = 2 * n;
+    return b;
+}
+
+__global__ void __launch_bounds__(kPairBlocksThreads, 1)
+linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
+                          const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 128, 128B swizzle
+                          const BlocksParams p) {
+    constexpr int S = kPairBlocksStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = ptx::smem_addr(smem_raw);
+    const uint32_t base = (raw_addr + 1023u) & ~1023u;
+    uint8_t* sm = smem_raw + (base - raw_addr);
+    constexpr uint32_t kBars = (uint32_t)(S * kPairBlocksStageBytes);
+    const uint32_t bar_full = base + kBars, bar_free = bar_full + 8u * S, bar_acc = bar_free + 8u * S, bar_acc_free = bar_acc + 16u,
+                   bar_drain = bar_acc_free + 16u;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + kBars + 8 * kPairBlocksBars);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kBars + 8 * kPairBlocksBars + 16);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    const bool leader = rank == 0;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S; ++i) {
+            ptx::mbar_init(bar_full + 8u * i, 1);
+            ptx::mbar_init(bar_free + 8u * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(bar_acc + 8u * i, 1);
+            ptx::mbar_init(bar_acc_free + 8u * i, 16);   // eight warps of each CTA
+        }
+        ptx::mbar_init(bar_drain, 1);
+        *abort_flag = 0u;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tensormap(&tmap_w);
+        ptx::prefetch_tensormap(&tmap_x);
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), 512);
+        ptx::tmem_relinquish_pair();
+    }
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    if (warp == 8 && p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync_all();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    const int token_tiles = p.offsets != nullptr ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
+    const int tiles = token_tiles * ((p.NB + 1) >> 1);
+    const int first = (int)blockIdx.x >> 1, step = (int)gridDim.x >> 1, KB = p.KB;
+    const int n_it = first < tiles ? ((tiles - first + step - 1) / step) * KB : 0;   // k-blocks of all tiles of this pair
+
+    if (warp == 8) {
+        // ------------------------------------------------------------------ loads (whole warp, one lane issues)
+        bool ok = true;
+        ptx::Ring r;
+        int issued = 0;
+        for (int i = first; i < tiles && ok; i += step) {
+            const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
+            const int y = (int)t.row + (int)rank * 128, n = t.nb * 128 + (int)rank * 128;
+            for (int b = 0; b < KB; ++b) {
+                if (issued >= S) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                const uint32_t full = bar_full + 8u * r.idx, to = ptx::map_to_cta(full, 0u), dst = base + (uint32_t)(r.idx * kPairBlocksStageBytes);
+                if (ptx::elect_one()) {
+                    if (leader) ptx::mbar_arrive_expect_tx(full, 2u * kPairBlocksStageBytes);
+                    ptx::tma_load_2d_pair(dst, &tmap_x, b * 128, y, to);
+                    ptx::tma_load_3d_pair(dst + 16384u, &tmap_w, b * 128, n, t.e, to);
+                }
+                r.advance(S);
+                ++issued;
+            }
+        }
+        if (!ok && leader && lane == 0) {   // gave up: let both CTAs' copies in flight land before either goes away
+            const uint64_t t0 = ptx::globaltimer_ns();
+            for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+                while (!ptx::mbar_try_wait(bar_full + 8u * (i % S), (uint32_t)((i / S) & 1)) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 20) {
+                }
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ MMAs (one lane of the leader issues)
+        if (leader) {
+            constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(256, 256);
+            bool ok = true;
+            ptx::Ring r, a;
+            for (int it = 0; it < n_it; ++it) {
+                if (it >= 2) ok = ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
+                ok = ok && ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t s = base + (uint32_t)(r.idx * kPairBlocksStageBytes);
+                const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
+                if (ptx::elect_one()) {
+                    ptx::umma_f8_kblock_pair(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
+                    if (it + S < n_it) ptx::umma_commit_pair(bar_free + 8u * r.idx, 3);   // (the slot is used again: see the closing barrier)
+                    ptx::umma_commit_pair(bar_acc + 8u * a.idx, 3);
+                }
+                r.advance(S);
+                a.advance(2);
+            }
+            if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
+                ptx::umma_commit_pair(bar_drain, 1);
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ sums and outputs: thread = token
+        const int q = warp & 3, half = warp >> 2;
+        const uint32_t src0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * 128);
+        bool ok = true;
+        ptx::Ring a;
+        int it = 0;
+        for (int i = first; i < tiles && ok; i += step) {
+            const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
+            const int at = (int)rank * 128 + q * 32 + lane, nb = t.nb + half;
+            const bool token = at < t.count && nb < p.NB;
+            const bool any = (int)rank * 128 + q * 32 < t.count && nb < p.NB;   // (warp-uniform)
+            const float* sx = p.s_x + (t.row + (token ? at : 0)) * p.lds;       // (a row that exists, for all threads)
+            const float* sw = p.s_w + ((int64_t)t.e * p.NB + (nb < p.NB ? nb : 0)) * KB;
+            unsigned long long acc[64];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) acc[j] = 0ull;
+            float next = __ldg(sx) * __ldg(sw);
+            for (int b = 0; b < KB; ++b, ++it) {
+                const unsigned long long f = pack_f32x2(next, next);
+                if (b + 1 < KB) next = __ldg(sx + b + 1) * __ldg(sw + b + 1);
+                ok = ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                if (any) {
+                    const uint32_t src = src0 + (uint32_t)(a.idx * 256);
+                    uint32_t v[2][16];
+                    ptx::tmem_ld_32x32b_x16(src, v[0]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        ptx::tmem_ld_wait_for(v[c & 1]);
+                        if (c < 7) ptx::tmem_ld_32x32b_x16(src + (uint32_t)(16 * c + 16), v[(c + 1) & 1]);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            acc[8 * c + j] = fma_f32x2(pack_f32x2(__uint_as_float(v[c & 1][2 * j]), __uint_as_float(v[c & 1][2 * j + 1])), f, acc[8 * c + j]);
+                    }
+                }
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0 && it + 2 < n_it) ptx::mbar_arrive_cluster(ptx::map_to_cta(bar_acc_free + 8u * a.idx, 0u));
+                a.advance(2);
+            }
+            if (ok && token) {
+                const int n = nb * 128, have = min(128, p.N - n);   // (a multiple of 16)
+                if (p.out_fp32) {
+                    float* y = static_cast<float*>(p.y) + (t.row + at) * p.ldy + n;
+                    const bool wide = (p.ldy & 3) == 0;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        float f[4];
+                        unpack_f32x2(acc[2 * j], f[0], f[1]);
+                        unpack_f32x2(acc[2 * j + 1], f[2], f[3]);
+                        if (4 * j >= have) break;
+                        if (wide) {
+                            *reinterpret_cast<float4*>(y + 4 * j) = make_float4(f[0], f[1], f[2], f[3]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) y[4 * j + k] = f[k];
+                        }
+                    }
+                } else {
+                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + (t.row + at) * p.ldy + n;
+                    const bool wide = (p.ldy & 7) == 0;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float lo, hi;
+                            unpack_f32x2(acc[4 * j + k], lo, hi);
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                            o[k] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        if (8 * j >= have) break;
+                        if (wide) {
+                            *reinterpret_cast<uint4*>(y + 8 * j) = make_uint4(o[0], o[1], o[2], o[3]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) reinterpret_cast<uint16_t*>(y)[8 * j + k] = (uint16_t)(o[k >> 1] >> (16 * (k & 1)));
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+        }
+    }
+
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    // Closing barrier: neither CTA leaves while the other may still reach into its shared memory or barriers.  What is sent to
+    // the other CTA has been waited for there: stages and freed buffers by the MMA warp (freed buffers are not announced after
+    // the last use), freed stages by the load warps (the same), complete buffers by the warps that add.
+    ptx::cluster_sync_all();
+    if (*abort_flag != 0u) {   // (not all of it, after a wait that gave up: late arrivals have 2 ms)
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 1000) {
+        }
+    }
+    __syncwarp();
+    if (warp == 9) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc_pair(tmem, 512);
+    }
 }
 
 }  // namespace w4a8
