@@ -398,13 +398,17 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
 // tokens and the sums of all 256 channels: 128 registers in each of 256 threads.  Its k-block's MMAs (512 cycles) go into one of two
 // buffers of tensor memory while the other is fetched (256 columns: 256 cycles) and added.
 //
-// Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs.
-constexpr int kPairBlocksThreads = 320, kPairBlocksStages = 6;
+// Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs, 10 scales (11 idle): the
+// products s_x * s_w of eight k-blocks at a time, through shared memory.  (Fetched by the warps that add, a k-block's scales cost
+// each of them a load of 32 lines, and its latency.)
+constexpr int kPairBlocksThreads = 384, kPairBlocksStages = 5;
+constexpr int kPairBlocksOutBytes = 8 * 4096;  // outputs on their way, 32 rows of 128 bytes per warp
+constexpr int kPairBlocksScaleBytes = 2 * 2 * kBlocksChunk * 128 * 4;   // [2 buffers][2 channel blocks][k-block][token]
 constexpr int kPairBlocksStageBytes = 32768;   // 128 tokens, 128 channels
 constexpr int kPairBlocksBand = 32;            // token tiles (8192 tokens) that share the channels' weights while they are in L2
-constexpr int kPairBlocksBars = 2 * kPairBlocksStages + 4 + 1;
+constexpr int kPairBlocksBars = 2 * kPairBlocksStages + 4 + 4 + 1;
 __host__ __device__ constexpr int pair_blocks_smem(bool grouped) {
-    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + 8 * kPairBlocksBars + 16 + (grouped ? (int)sizeof(ExpertTable) : 0);
+    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + kPairBlocksScaleBytes + kPairBlocksOutBytes + 8 * kPairBlocksBars + 16 + (grouped ? (int)sizeof(ExpertTable) : 0);
 }
 
 // Tile index -> expert, pair of channel blocks and rows.
@@ -433,9 +437,10 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     const uint32_t base = (raw_addr + 1023u) & ~1023u;
     uint8_t* sm = smem_raw + (base - raw_addr);
-    constexpr uint32_t kBars = (uint32_t)(S * kPairBlocksStageBytes);
+    constexpr uint32_t kScales = (uint32_t)(S * kPairBlocksStageBytes), kOut = kScales + (uint32_t)kPairBlocksScaleBytes,
+                       kBars = kOut + (uint32_t)kPairBlocksOutBytes;
     const uint32_t bar_full = base + kBars, bar_free = bar_full + 8u * S, bar_acc = bar_free + 8u * S, bar_acc_free = bar_acc + 16u,
-                   bar_drain = bar_acc_free + 16u;
+                   bar_scales = bar_acc_free + 16u, bar_scales_free = bar_scales + 16u, bar_drain = bar_scales_free + 16u;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + kBars + 8 * kPairBlocksBars);
     volatile uint32_t* abort_flag = tmem_slot + 1;
     ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kBars + 8 * kPairBlocksBars + 16);
@@ -451,6 +456,8 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(bar_acc + 8u * i, 1);
             ptx::mbar_init(bar_acc_free + 8u * i, 16);   // eight warps of each CTA
+            ptx::mbar_init(bar_scales + 8u * i, 1);
+            ptx::mbar_init(bar_scales_free + 8u * i, 8);
         }
         ptx::mbar_init(bar_drain, 1);
         *abort_flag = 0u;
@@ -477,6 +484,8 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
 
     if (warp == 8) {
         // ------------------------------------------------------------------ loads (whole warp, one lane issues)
+        // (registers: 64 x 128 + 216 x 256 threads of the 168 x 384 that the block is launched with)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         bool ok = true;
         ptx::Ring r;
         int issued = 0;
@@ -505,21 +514,23 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         __syncwarp();
     } else if (warp == 9) {
         // ------------------------------------------------------------------ MMAs (one lane of the leader issues)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (leader) {
             constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(256, 256);
             bool ok = true;
             ptx::Ring r, a;
             for (int it = 0; it < n_it; ++it) {
-                if (it >= 2) ok = ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
-                ok = ok && ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+                // (the buffer is waited for last: it is what comes last)
+                ok = ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+                if (it >= 2) ok = ok && ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t s = base + (uint32_t)(r.idx * kPairBlocksStageBytes);
                 const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
                 if (ptx::elect_one()) {
                     ptx::umma_f8_kblock_pair(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
-                    if (it + S < n_it) ptx::umma_commit_pair(bar_free + 8u * r.idx, 3);   // (the slot is used again: see the closing barrier)
                     ptx::umma_commit_pair(bar_acc + 8u * a.idx, 3);
+                    if (it + S < n_it) ptx::umma_commit_pair(bar_free + 8u * r.idx, 3);   // (the slot is used again: see the closing barrier)
                 }
                 r.advance(S);
                 a.advance(2);
@@ -532,90 +543,190 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
             }
         }
         __syncwarp();
-    } else {
-        // ------------------------------------------------------------------ sums and outputs: thread = token
-        const int q = warp & 3, half = warp >> 2;
-        const uint32_t src0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * 128);
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ scales (a lane has four tokens)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         bool ok = true;
-        ptx::Ring a;
-        int it = 0;
+        ptx::Ring r;
+        int filled = 0;
+        const bool wide = (p.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(p.s_x) & 15u) == 0;
         for (int i = first; i < tiles && ok; i += step) {
             const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
-            const int at = (int)rank * 128 + q * 32 + lane, nb = t.nb + half;
-            const bool token = at < t.count && nb < p.NB;
-            const bool any = (int)rank * 128 + q * 32 < t.count && nb < p.NB;   // (warp-uniform)
-            const float* sx = p.s_x + (t.row + (token ? at : 0)) * p.lds;       // (a row that exists, for all threads)
-            const float* sw = p.s_w + ((int64_t)t.e * p.NB + (nb < p.NB ? nb : 0)) * KB;
+            const float* sw0 = p.s_w + ((int64_t)t.e * p.NB + t.nb) * KB;
+            const float* sw1 = t.nb + 1 < p.NB ? sw0 + KB : sw0;
+            for (int b0 = 0; b0 < KB; b0 += kBlocksChunk) {
+                float w0 = 0.0f, w1 = 0.0f;
+                const int n = min(kBlocksChunk, KB - b0);
+                if (lane < n) {
+                    w0 = __ldg(sw0 + b0 + lane);
+                    w1 = __ldg(sw1 + b0 + lane);
+                }
+                if (filled >= 2) ok = ptx::mbar_wait_warp(bar_scales_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                float* f = reinterpret_cast<float*>(sm + kScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
+#pragma unroll 2
+                for (int k = 0; k < 4; ++k) {
+                    const int in = (int)rank * 128 + k * 32 + lane;
+                    const float* sx = p.s_x + (t.row + min(in, t.count - 1)) * p.lds + b0;   // (a row that exists)
+                    float x[kBlocksChunk];
+                    if (wide && n == kBlocksChunk) {
+                        const float4 u = __ldg(reinterpret_cast<const float4*>(sx)), v = __ldg(reinterpret_cast<const float4*>(sx) + 1);
+                        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kBlocksChunk; ++j) x[j] = j < n ? __ldg(sx + j) : 0.0f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBlocksChunk; ++j) {
+                        f[j * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w0, j);
+                        f[(kBlocksChunk + j) * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w1, j);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_scales + 8u * r.idx);
+                r.advance(2);
+                ++filled;
+            }
+        }
+        __syncwarp();
+    } else if (warp == 11) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    } else {
+        // ------------------------------------------------------------------ sums and outputs: thread = token
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // (128 registers of sums and 64 of columns leave few: the loop over k-blocks keeps next to nothing, and what is needed
+        // around it is worked out again.  With spills in it, it took a third longer.)
+        const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
+        const uint32_t sc_mine = base + kScales + (uint32_t)((warp >> 2) * kBlocksChunk * 512 + (warp & 3) * 128 + lane * 4);
+        bool ok = true;
+        int it = 0, chunk = 0;   // k-blocks and chunks of eight of them so far
+        for (int i = first; i < tiles && ok; i += step) {
+            bool any;   // (warp-uniform) a token of this warp, and its channels, are there
+            {
+                const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
+                any = (int)rank * 128 + (warp & 3) * 32 < t.count && t.nb + (warp >> 2) < p.NB;
+            }
             unsigned long long acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = 0ull;
-            float next = __ldg(sx) * __ldg(sw);
-            for (int b = 0; b < KB; ++b, ++it) {
-                const unsigned long long f = pack_f32x2(next, next);
-                if (b + 1 < KB) next = __ldg(sx + b + 1) * __ldg(sw + b + 1);
-                ok = ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
+            for (int left = p.KB; left > 0 && ok; ++chunk) {
+                ok = ptx::mbar_wait_warp(bar_scales + 8u * (chunk & 1), (uint32_t)(chunk >> 1) & 1u, abort_flag, p.status);
                 if (!ok) break;
-                ptx::tc_fence_after_sync();
-                if (any) {
-                    const uint32_t src = src0 + (uint32_t)(a.idx * 256);
-                    uint32_t v[2][16];
-                    ptx::tmem_ld_32x32b_x16(src, v[0]);
+                const uint32_t sc = sc_mine + (uint32_t)((chunk & 1) * 2 * kBlocksChunk * 512);
+                const int end = min(kBlocksChunk, left);
+                left -= end;
+#pragma unroll 1
+                for (int j = 0; j < end; ++j, ++it) {
+                    float fs;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(fs) : "r"(sc + (uint32_t)(j * 512)) : "memory");
+                    ok = ptx::mbar_wait_warp(bar_acc + 8u * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    const unsigned long long f = pack_f32x2(fs, fs);
+                    auto release = [&]() {   // the buffer has been read
+                        ptx::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0 && it + 2 < n_it) ptx::mbar_arrive_cluster(ptx::map_to_cta(bar_acc_free + 8u * (it & 1), 0u));
+                    };
+                    if (any) {
+                        // 32 columns are on their way while those before are added
+                        const uint32_t from = src + (uint32_t)((it & 1) * 256);
+                        uint32_t v[2][2][16];
+                        ptx::tmem_ld_32x32b_x16(from, v[0][0]);
+                        ptx::tmem_ld_32x32b_x16(from + 16u, v[0][1]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        ptx::tmem_ld_wait_for(v[c & 1]);
-                        if (c < 7) ptx::tmem_ld_32x32b_x16(src + (uint32_t)(16 * c + 16), v[(c + 1) & 1]);
+                        for (int c = 0; c < 4; ++c) {
+                            ptx::tmem_ld_wait_for(v[c & 1][0], v[c & 1][1]);
+                            if (c < 3) {
+                                ptx::tmem_ld_32x32b_x16(from + (uint32_t)(32 * c + 32), v[(c + 1) & 1][0]);
+                                ptx::tmem_ld_32x32b_x16(from + (uint32_t)(32 * c + 48), v[(c + 1) & 1][1]);
+                            } else {
+                                release();
+                            }
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            acc[8 * c + j] = fma_f32x2(pack_f32x2(__uint_as_float(v[c & 1][2 * j]), __uint_as_float(v[c & 1][2 * j + 1])), f, acc[8 * c + j]);
+                            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    acc[16 * c + 8 * z + k] =
+                                        fma_f32x2(pack_f32x2(__uint_as_float(v[c & 1][z][2 * k]), __uint_as_float(v[c & 1][z][2 * k + 1])), f, acc[16 * c + 8 * z + k]);
+                        }
+                    } else {
+                        release();
                     }
                 }
-                ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0 && it + 2 < n_it) ptx::mbar_arrive_cluster(ptx::map_to_cta(bar_acc_free + 8u * a.idx, 0u));
-                a.advance(2);
+                if (lane == 0) ptx::mbar_arrive(bar_scales_free + 8u * (chunk & 1));
             }
-            if (ok && token) {
-                const int n = nb * 128, have = min(128, p.N - n);   // (a multiple of 16)
-                if (p.out_fp32) {
-                    float* y = static_cast<float*>(p.y) + (t.row + at) * p.ldy + n;
-                    const bool wide = (p.ldy & 3) == 0;
+            if (ok && any) {
+                // Outputs, 128 bytes of 32 rows at a time, through shared memory (pieces of 16 bytes permuted by their row, so that
+                // neither side meets a bank twice): a store then touches four lines, not one for each of 32 rows.
+                const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
+                const int q = warp & 3, nb = t.nb + (warp >> 2);
+                const uint32_t out_s = base + kOut + (uint32_t)(warp * 4096);
+                const int es = p.out_fp32 ? 4 : 2;
+                const bool wide = ((p.ldy * es) & 15) == 0;   // rows 16-byte aligned (y itself is)
+                const int row0 = (int)rank * 128 + q * 32, rows = min(32, t.count - row0);
+                uint8_t* y0 = static_cast<uint8_t*>(p.y) + ((t.row + row0) * p.ldy + nb * 128) * es;
+                const int have = min(128, p.N - nb * 128) * es;   // bytes of a row of this channel block
+                auto store = [&](int piece) {   // the piece's rows, four of them per round
+                    __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float f[4];
-                        unpack_f32x2(acc[2 * j], f[0], f[1]);
-                        unpack_f32x2(acc[2 * j + 1], f[2], f[3]);
-                        if (4 * j >= have) break;
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = 4 * k + (lane >> 3), byte = piece * 128 + (lane & 7) * 16;
+                        uint4 o;
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w)
+                                     : "r"(out_s + (uint32_t)(row * 128 + (((lane ^ row) & 7) << 4)))
+                                     : "memory");
+                        if (row >= rows || byte >= have) continue;
+                        uint8_t* to = y0 + (int64_t)row * p.ldy * es + byte;
                         if (wide) {
-                            *reinterpret_cast<float4*>(y + 4 * j) = make_float4(f[0], f[1], f[2], f[3]);
-                        } else {
+                            *reinterpret_cast<uint4*>(to) = o;
+                        } else if (es == 4) {
+                            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) y[4 * j + k] = f[k];
+                            for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(to)[i] = w[i];
+                        } else {
+                            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
                         }
+                    }
+                    __syncwarp();
+                };
+                const uint32_t mine = out_s + (uint32_t)(lane * 128);
+                if (p.out_fp32) {
+#pragma unroll
+                    for (int piece = 0; piece < 4; ++piece) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            float f[4];
+                            unpack_f32x2(acc[16 * piece + 2 * c], f[0], f[1]);
+                            unpack_f32x2(acc[16 * piece + 2 * c + 1], f[2], f[3]);
+                            ptx::st_shared_v4(mine + (uint32_t)(((c ^ lane) & 7) << 4),
+                                              make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+                        }
+                        store(piece);
                     }
                 } else {
-                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + (t.row + at) * p.ldy + n;
-                    const bool wide = (p.ldy & 7) == 0;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        uint32_t o[4];
+                    for (int piece = 0; piece < 2; ++piece) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            float lo, hi;
-                            unpack_f32x2(acc[4 * j + k], lo, hi);
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                            o[k] = *reinterpret_cast<const uint32_t*>(&h);
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float lo, hi;
+                                unpack_f32x2(acc[32 * piece + 4 * c + k], lo, hi);
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                                o[k] = *reinterpret_cast<const uint32_t*>(&h);
+                            }
+                            ptx::st_shared_v4(mine + (uint32_t)(((c ^ lane) & 7) << 4), make_uint4(o[0], o[1], o[2], o[3]));
                         }
-                        if (8 * j >= have) break;
-                        if (wide) {
-                            *reinterpret_cast<uint4*>(y + 8 * j) = make_uint4(o[0], o[1], o[2], o[3]);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) reinterpret_cast<uint16_t*>(y)[8 * j + k] = (uint16_t)(o[k >> 1] >> (16 * (k & 1)));
-                        }
+                        store(piece);
                     }
                 }
             }
-            __syncwarp();
         }
     }
 

@@ -452,6 +452,11 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
                  :
                  : "memory");
 }
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&a)[16], uint32_t (&b)[16]) {
+    tmem_ld_wait_for(a);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(b[i]));
+}
 // 16 lanes x 16 consecutive 32-bit columns as two fragments of eight columns: of fragment f thread t receives lane
 // t / 4, columns 2 (t % 4) and the next in r[4 f], r[4 f + 1] and lane t / 4 + 8 in r[4 f + 2], r[4 f + 3].
 __device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) {
