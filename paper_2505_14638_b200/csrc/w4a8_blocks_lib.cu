@@ -169,21 +169,18 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
 }
 
 // ------------------------------------------------------------------------------ routing
-// Up to a token per warp of a cluster: one launch.
-static bool route_clustered(int64_t M) { return M <= kRouteCluster * kRouteWarps; }
-
+// Whole clusters of CTAs; up to a token per warp of a cluster: a single one.
 static void route_chunks(int64_t M, int* chunk, int* chunks) {
-    int64_t per = ceil_div(M, route_clustered(M) ? kRouteCluster : kRouteChunks);
-    if (!route_clustered(M) && per < kRouteWarps) per = kRouteWarps;
+    int64_t per = ceil_div(M, M <= kRouteCluster * kRouteWarps ? kRouteCluster : kRouteChunks);
+    if (M > kRouteCluster * kRouteWarps && per < kRouteWarps) per = kRouteWarps;
     *chunk = (int)per;
-    *chunks = (int)ceil_div(M, per);
+    *chunks = (int)(ceil_div(ceil_div(M, per), kRouteCluster) * kRouteCluster);
 }
 
 template <int V>
 static int launch_choose(const RouteParams& p, bool wide, cudaStream_t st) {
-    const int cluster = p.clustered ? p.chunks : 1;
-    return wide ? launch(route_choose_kernel<V, uint64_t>, (unsigned)p.chunks, kRouteWarps * 32, 0, cluster, st, p)
-                : launch(route_choose_kernel<V, uint32_t>, (unsigned)p.chunks, kRouteWarps * 32, 0, cluster, st, p);
+    return wide ? launch(route_choose_kernel<V, true>, (unsigned)p.chunks, kRouteWarps * 32, 0, kRouteCluster, st, p)
+                : launch(route_choose_kernel<V, false>, (unsigned)p.chunks, kRouteWarps * 32, 0, kRouteCluster, st, p);
 }
 
 }  // namespace w4a8
@@ -213,7 +210,7 @@ size_t w4a8_route_experts_workspace_bytes(int64_t M, int64_t experts) {
     if (M <= 0 || experts <= 0 || experts > kRouteMaxExperts) return 0;
     int chunk, chunks;
     route_chunks(M, &chunk, &chunks);
-    return !route_clustered(M) ? (size_t)chunks * (size_t)experts * sizeof(uint32_t) : 0;
+    return chunks > kRouteCluster ? (size_t)(chunks / kRouteCluster) * (size_t)experts * sizeof(uint32_t) : 0;
 }
 
 int w4a8_route_experts(const void* logits, int logits_dtype, int64_t M, int64_t ldl, int64_t experts, int top_k, int score,
@@ -256,14 +253,13 @@ int w4a8_route_experts(const void* logits, int logits_dtype, int64_t M, int64_t 
     p.renormalize = renormalize;
     p.scale = scale;
     route_chunks(M, &p.chunk, &p.chunks);
-    p.clustered = route_clustered(M) ? 1 : 0;
     const bool wide = bias != nullptr || (groups > 1 && group_best == 2);
     if (experts <= 32) rc = launch_choose<1>(p, wide, st);
     else if (experts <= 64) rc = launch_choose<2>(p, wide, st);
     else if (experts <= 128) rc = launch_choose<4>(p, wide, st);
     else if (experts <= 256) rc = launch_choose<8>(p, wide, st);
     else rc = launch_choose<16>(p, wide, st);
-    if (rc != W4A8_OK || p.clustered) return rc;
+    if (rc != W4A8_OK || p.chunks == kRouteCluster) return rc;
     return launch(route_place_kernel, (unsigned)p.chunks, kRouteWarps * 32, 0, 1, st, p);
 }
 

@@ -1,20 +1,21 @@
 // Routing of tokens to experts: the choice of top_k experts from router logits, their weights, and the order of the rows by
 // expert that the experts' products read.
 //
-// route_choose_kernel: a warp per token, V consecutive experts per lane; then the CTA counts its tokens' experts and numbers the rows
-// of each expert in the order of the tokens.  Up to 128 tokens the CTAs are one cluster and read one another's counts: one launch.
-// Above, route_place_kernel follows: every CTA sums the counts of the CTAs before it (at most kRouteChunks rows, from L2) and turns
-// the numbers into rows.  No atomics: the order never varies.
+// route_choose_kernel: clusters of eight CTAs, a warp per token, V consecutive experts per lane; then a CTA counts its tokens'
+// experts, numbers the rows of each expert in the order of the tokens and tells the other CTAs of the cluster its counts.  Up to
+// 128 tokens that is all: one cluster, one launch.  Above, route_place_kernel follows: every CTA sums the counts of the clusters
+// before its own (at most 36 rows, from L2) and turns the numbers into rows.  No atomics on global memory: the order never varies.
 //
 // Nothing here is near the bound of its bytes (2 MB of logits: 0.4 us): what counts are launches and the length of the chain of
-// dependent steps of a token -- load, keys, groups, top_k rounds of a warp-wide maximum, weights.  Hence: groups judged all
-// at once by exchanges among the lanes that hold them; a maximum of 64-bit keys by their upper words, by the lower ones only
-// where those are equal; weights in FP64 for as many of a warp's tokens at a time as fill its lanes; the next token's logits
-// fetched ahead.
+// dependent steps of a token -- load, keys, groups, top_k rounds of a warp-wide maximum, weights.  Hence: a key carries its
+// expert's index in its low bits, so that no two are equal and a maximum says whose it is; a lane sorts its keys once and
+// gives up the first (looking for the next one among eight took 525 cycles a round, this takes 150); groups are judged all at
+// once by exchanges among the lanes that hold them; weights in FP64 for as many of a warp's tokens at a time as fill its lanes;
+// the next token's logits are fetched ahead.
 //
 // The choice: without a bias and with groups judged by their best expert, scores have the order of the logits, whose 32 bits are
-// the keys.  Otherwise a key is score + bias in FP64: in FP32 two experts whose keys differ by less than a rounding would
-// change places.
+// the keys' upper words.  Otherwise (WIDE) a key is score + bias in FP64, cut to 43 bits of fraction: in FP32 two experts whose
+// keys differ by less than a rounding would change places.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -26,8 +27,8 @@ namespace w4a8 {
 
 constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 32, kRouteMaxGroups = 32;
 constexpr int kRouteWarps = 16;      // tokens that a CTA works on at a time
-constexpr int kRouteChunks = 148;    // CTAs at most
-constexpr int kRouteCluster = 8;     // CTAs of the single launch
+constexpr int kRouteCluster = 8;
+constexpr int kRouteChunks = 288;    // CTAs at most: two per SM
 constexpr int kRouteLocalIds = 2048; // choices of a CTA that are kept in shared memory
 
 struct RouteParams {
@@ -36,30 +37,56 @@ struct RouteParams {
     const float* bias;
     int32_t *ids, *offsets, *slots;
     float* weights;
-    uint32_t* counts;   // [chunks][E]
+    uint32_t* counts;   // [clusters][E]
     int64_t M;
     int E, top_k, groups, top_groups, group_best, chunk, chunks;
-    int logits_fp32, sigmoid, renormalize, clustered;
+    int logits_fp32, sigmoid, renormalize;
     float scale;
 };
 
-// Keys whose order as unsigned integers is that of the values; 0 is left for experts that cannot be chosen.
-__device__ __forceinline__ uint64_t order_key(double v) {
+// Keys: their order as unsigned integers is that of the values, and for equal values the lower index comes first; 0 is left for
+// experts that cannot be chosen.
+constexpr uint64_t kRouteIndexBits = 511u;
+static_assert(kRouteMaxExperts == kRouteIndexBits + 1, "an index fits the low bits");
+__device__ __forceinline__ uint64_t order_bits(double v) {
     const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);   // (-0 becomes 0)
     return b ^ ((b >> 63) ? 0xFFFFFFFFFFFFFFFFull : 0x8000000000000000ull);
 }
-__device__ __forceinline__ uint32_t order_key(float v) {
+__device__ __forceinline__ uint32_t order_bits(float v) {
     const uint32_t b = __float_as_uint(v + 0.0f);
     return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
+__device__ __forceinline__ uint64_t route_key(double v, int e) { return (order_bits(v) & ~kRouteIndexBits) | (kRouteIndexBits - (uint64_t)e); }
+__device__ __forceinline__ uint64_t route_key(float v, int e) { return (uint64_t)order_bits(v) << 32 | (kRouteIndexBits - (uint64_t)e); }
+__device__ __forceinline__ int key_index(uint64_t k) { return (int)(kRouteIndexBits - (k & kRouteIndexBits)); }
 __device__ __forceinline__ double key_value(uint64_t k) {
+    k &= ~kRouteIndexBits;
     return __longlong_as_double((long long)(k ^ ((k >> 63) ? 0x8000000000000000ull : 0xFFFFFFFFFFFFFFFFull)));
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t k) { return __reduce_max_sync(0xFFFFFFFFu, k); }
 __device__ __forceinline__ uint64_t warp_max(uint64_t k) {
     const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(k >> 32));
     const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
     return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
+
+// Batcher's odd-even merge sort, descending (V a power of two, at most 16).
+template <int V>
+__device__ __forceinline__ void sort_keys(uint64_t (&k)[V]) {
+#pragma unroll
+    for (int p = 1; p < V; p <<= 1)
+#pragma unroll
+        for (int q = p; q >= 1; q >>= 1)
+#pragma unroll
+            for (int j = q % p; j + q < V; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                        const uint64_t a = k[i + j], b = k[i + j + q];
+                        k[i + j] = max64(a, b);
+                        k[i + j + q] = min64(a, b);
+                    }
 }
 
 __device__ __forceinline__ float route_logit(const RouteParams& p, int64_t at) {
@@ -127,32 +154,31 @@ __device__ __forceinline__ void route_load(const RouteParams& p, int64_t m, int 
         if (x[i] != x[i]) x[i] = -INFINITY;
 }
 
-template <int V, typename Key>
+template <int V, bool WIDE>
 __global__ void __launch_bounds__(kRouteWarps * 32)
 route_choose_kernel(const RouteParams p) {
-    constexpr bool WIDE = sizeof(Key) == 8;
-    __shared__ uint32_t count[kRouteMaxExperts], total[kRouteMaxExperts], first[kRouteMaxExperts + 1], sums[kRouteWarps];
+    __shared__ uint32_t count[kRouteMaxExperts], from[kRouteCluster][kRouteMaxExperts], first[kRouteMaxExperts + 1], sums[kRouteWarps];
     __shared__ __align__(16) uint8_t warp_count[kRouteWarps][kRouteMaxExperts];
     __shared__ int16_t local_ids[kRouteLocalIds];
     ptx::griddep_launch_dependents();
-    ptx::griddep_wait();
+    ptx::cluster_arrive_relaxed();   // (waited for ahead of the first access to another CTA's shared memory: all have started by then)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e0 = lane * V;
     const int E = p.E, k = p.top_k, size = E / p.groups;
-    const int64_t m0 = (int64_t)blockIdx.x * p.chunk, m1 = min(p.M, m0 + p.chunk);
+    const int64_t m0 = min(p.M, (int64_t)blockIdx.x * p.chunk), m1 = min(p.M, m0 + p.chunk);
     const bool local = (int64_t)p.chunk * k <= kRouteLocalIds;
-    for (int e = threadIdx.x; e < E; e += kRouteWarps * 32) count[e] = 0u;
+    const uint32_t rank = ptx::cluster_ctarank();
+    if ((int)threadIdx.x < E) count[threadIdx.x] = 0u;
     // lanes of a group, where a group is a power of two of whole lanes; 0 otherwise
     const int span = size % V == 0 && ((size / V) & (size / V - 1)) == 0 ? size / V : 0;
-    float bias[WIDE ? V : 1];
+    // A warp's tokens are weighed `batch` at a time, each by kp lanes.
+    const int kp = k <= 1 ? 1 : 1 << (32 - __clz(k - 1)), batch = 32 / kp, sub = lane / kp, j_mine = lane & (kp - 1);
+    ptx::griddep_wait();
+    float ahead[V], bias[WIDE ? V : 1];
+    if (m0 + warp < m1) route_load<V>(p, m0 + warp, e0, ahead);
     if constexpr (WIDE) {
 #pragma unroll
         for (int i = 0; i < V; ++i) bias[i] = p.bias != nullptr && e0 + i < E ? __ldg(p.bias + e0 + i) : 0.0f;
     }
-    // A warp's tokens are weighed `batch` at a time, each by kp lanes.
-    const int kp = k <= 1 ? 1 : 1 << (32 - __clz(k - 1)), batch = 32 / kp, sub = lane / kp, j_mine = lane & (kp - 1);
-
-    float ahead[V];
-    if (m0 + warp < m1) route_load<V>(p, m0 + warp, e0, ahead);
     for (int64_t mb = m0 + warp; mb < m1; mb += (int64_t)batch * kRouteWarps) {
         int id = -1;                             // lane sub * kp + j: choice j of the batch's token sub
         float most_mine = 0.0f;                  // that token's largest logit
@@ -173,7 +199,7 @@ route_choose_kernel(const RouteParams p) {
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
             }
-            Key key[V];
+            uint64_t key[V];
             if constexpr (WIDE) {
                 double s[V];
 #pragma unroll
@@ -185,20 +211,18 @@ route_choose_kernel(const RouteParams p) {
                         sum64 += s[i];
                     }
                 }
-                double scale = 1.0;
                 if (!p.sigmoid) {
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) sum64 += __shfl_xor_sync(0xFFFFFFFFu, sum64, o);
-                    scale = sum64;
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const double v = (p.sigmoid ? s[i] : s[i] / scale) + (double)bias[i];
-                    key[i] = x[i] == -INFINITY || !(v > -(double)INFINITY) ? 0 : order_key(v);
+                    const double v = (p.sigmoid ? s[i] : s[i] / sum64) + (double)bias[i];
+                    key[i] = x[i] == -INFINITY || !(v > -(double)INFINITY) ? 0 : route_key(v, e0 + i);
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) key[i] = x[i] == -INFINITY ? 0 : order_key(x[i]);
+                for (int i = 0; i < V; ++i) key[i] = x[i] == -INFINITY ? 0 : route_key(x[i], e0 + i);
                 if (!p.sigmoid && !p.renormalize) {
                     float sum = 0.0f;
 #pragma unroll
@@ -214,34 +238,31 @@ route_choose_kernel(const RouteParams p) {
             }
 
             if (p.groups > 1) {
-                // A group's key: the sum of the group_best highest, lowest where one of them cannot be chosen.
-                auto judge = [&](Key top, Key next) -> Key {
-                    if constexpr (WIDE) {
-                        if (p.group_best == 2 && size > 1) return top == 0 || next == 0 ? 0 : order_key(key_value(top) + key_value(next));
-                    }
-                    return top;
+                // A group's key: the sum of the group_best highest, lowest where one of them cannot be chosen.  (An index in its low
+                // bits does no harm: groups of equal value are taken in their order, which is that of their best experts' indices
+                // as long as these are not compared; so they are taken off.)
+                auto judge = [&](uint64_t top, uint64_t next) -> uint64_t {
+                    if (WIDE && p.group_best == 2 && size > 1) return top == 0 || next == 0 ? 0 : order_bits(key_value(top) + key_value(next));
+                    return top == 0 ? 0 : top | kRouteIndexBits;
                 };
-                unsigned kept = 0;
                 if (span > 0) {
-                    Key best = 0, second = 0;
+                    uint64_t best = 0, second = 0;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const Key low = key[i] < best ? key[i] : best;
-                        best = key[i] > best ? key[i] : best;
-                        second = low > second ? low : second;
+                        second = max64(second, min64(key[i], best));
+                        best = max64(best, key[i]);
                     }
                     for (int o = 1; o < span; o <<= 1) {   // (lanes of one group exchange theirs)
-                        const Key b2 = __shfl_xor_sync(0xFFFFFFFFu, best, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, second, o);
-                        const Key low = b2 < best ? b2 : best;
-                        best = b2 > best ? b2 : best;
-                        second = second > s2 ? second : s2;
-                        second = low > second ? low : second;
+                        const uint64_t b2 = __shfl_xor_sync(0xFFFFFFFFu, best, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, second, o);
+                        second = max64(max64(second, s2), min64(best, b2));
+                        best = max64(best, b2);
                     }
-                    const Key score = judge(best, second);
+                    const uint64_t score = judge(best, second);
                     const int mine = lane / span;
                     int before = 0;   // groups that come before this lane's
+#pragma unroll 8
                     for (int g = 0; g < p.groups; ++g) {
-                        const Key other = __shfl_sync(0xFFFFFFFFu, score, g * span);
+                        const uint64_t other = __shfl_sync(0xFFFFFFFFu, score, g * span);
                         before += other > score || (other == score && g < mine) ? 1 : 0;
                     }
                     if (mine >= p.groups || before >= p.top_groups) {
@@ -249,69 +270,40 @@ route_choose_kernel(const RouteParams p) {
                         for (int i = 0; i < V; ++i) key[i] = 0;
                     }
                 } else {
-                    Key score = 0;   // lane g judges group g
+                    uint64_t score = 0;   // lane g judges group g
                     for (int g = 0; g < p.groups; ++g) {
-                        Key best = 0, second = 0;   // this lane's in the group
+                        uint64_t best = 0, second = 0;   // this lane's in the group
 #pragma unroll
                         for (int i = 0; i < V; ++i) {
                             if (e0 + i < g * size || e0 + i >= (g + 1) * size) continue;
-                            const Key low = key[i] < best ? key[i] : best;
-                            best = key[i] > best ? key[i] : best;
-                            second = low > second ? low : second;
+                            second = max64(second, min64(key[i], best));
+                            best = max64(best, key[i]);
                         }
-                        const Key top = warp_max(best);
-                        const unsigned holds = __ballot_sync(0xFFFFFFFFu, best == top);
-                        const Key next = warp_max(lane == __ffs((int)holds) - 1 ? second : best);
+                        const uint64_t top = warp_max(best), next = warp_max(best == top ? second : best);
                         if (lane == g) score = judge(top, next);
                     }
                     int before = 0;
                     for (int g = 0; g < p.groups; ++g) {
-                        const Key other = __shfl_sync(0xFFFFFFFFu, score, g);
+                        const uint64_t other = __shfl_sync(0xFFFFFFFFu, score, g);
                         before += other > score || (other == score && g < lane) ? 1 : 0;
                     }
-                    kept = __ballot_sync(0xFFFFFFFFu, lane < p.groups && before < p.top_groups);
+                    const unsigned kept = __ballot_sync(0xFFFFFFFFu, lane < p.groups && before < p.top_groups);
 #pragma unroll
                     for (int i = 0; i < V; ++i)
                         if (e0 + i < E && !(kept >> ((e0 + i) / size) & 1u)) key[i] = 0;
                 }
             }
 
-            // The choices, highest first: the lane with the highest key of all gives it up and looks for its next one.
-            Key best = 0;
-            int at = 0;
-            auto own_best = [&]() {
-                best = 0;
-                at = 0;
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (key[i] > best) {
-                        best = key[i];
-                        at = i;
-                    }
-            };
-            own_best();
+            // The choices, highest first.
+            sort_keys<V>(key);
             for (int j = 0; j < k; ++j) {
-                unsigned holds;
-                if constexpr (WIDE) {
-                    const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(best >> 32));
-                    holds = __ballot_sync(0xFFFFFFFFu, (uint32_t)(best >> 32) == hi);
-                    if ((holds & (holds - 1u)) != 0u) {
-                        const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, (holds >> lane & 1u) ? (uint32_t)best : 0u);
-                        holds = __ballot_sync(0xFFFFFFFFu, (holds >> lane & 1u) && (uint32_t)best == lo);
-                    }
-                } else {
-                    const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, best);
-                    holds = __ballot_sync(0xFFFFFFFFu, best == top);
-                }
-                const int from = __ffs((int)holds) - 1;   // (equal keys: the lowest lane has the lowest index)
-                const int e = __shfl_sync(0xFFFFFFFFu, best == 0 ? -1 : e0 + at, from);
-                if (e < 0) break;
-                if (lane == b * kp + j) id = e;
-                if (lane == from) {
+                const uint64_t top = warp_max(key[0]);
+                if (top == 0) break;
+                if (lane == b * kp + j) id = key_index(top);
+                if (key[0] == top) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (i == at) key[i] = 0;
-                    own_best();
+                    for (int i = 0; i + 1 < V; ++i) key[i] = key[i + 1];
+                    key[V - 1] = 0;
                 }
             }
         }
@@ -337,61 +329,72 @@ route_choose_kernel(const RouteParams p) {
     }
 
     // Rows of each expert among this CTA's tokens, numbered in their order: 512 choices at a time, a warp's 32 among themselves and
-    // then behind those of the warps before it.
+    // then behind those of the warps before it.  The last (or only) round's numbers stay in registers.
     const int64_t begin = m0 * k, end = m1 * k;
-    for (int64_t i0 = begin; i0 < end; i0 += kRouteWarps * 32) {
-        for (int c = threadIdx.x; c < kRouteWarps * kRouteMaxExperts / 16; c += kRouteWarps * 32)
-            reinterpret_cast<uint4*>(&warp_count[0][0])[c] = make_uint4(0u, 0u, 0u, 0u);
+    int e = -1;
+    uint32_t number = 0;
+    int64_t i0 = begin;
+    while (true) {
+        const int used = (int)min((int64_t)kRouteWarps, (end - i0 + 31) / 32);   // warps with choices
+        if (warp < used) {
+#pragma unroll
+            for (int c = lane; c < kRouteMaxExperts / 16; c += 32) reinterpret_cast<uint4*>(warp_count[warp])[c] = make_uint4(0u, 0u, 0u, 0u);
+        }
         __syncthreads();
         const int64_t i = i0 + threadIdx.x;
-        const int e = i < end ? (local ? (int)local_ids[i - begin] : __ldcg(p.ids + i)) : -1;
+        e = i < end ? (local ? (int)local_ids[i - begin] : __ldcg(p.ids + i)) : -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
         if (e >= 0 && (same >> lane) == 1u) warp_count[warp][e] = (uint8_t)__popc(same);   // (the last of them)
         __syncthreads();
-        uint32_t rank = 0, had = 0;
         if (e >= 0) {
-            rank = count[e] + __popc(same & ((1u << lane) - 1u));
-            for (int w = 0; w < warp; ++w) rank += warp_count[w][e];
+            number = count[e] + __popc(same & ((1u << lane) - 1u));
+            for (int w = 0; w < warp; ++w) number += warp_count[w][e];
         }
+        uint32_t had = 0;
         if ((int)threadIdx.x < E)
-#pragma unroll
-            for (int w = 0; w < kRouteWarps; ++w) had += warp_count[w][threadIdx.x];
+            for (int w = 0; w < used; ++w) had += warp_count[w][threadIdx.x];
         __syncthreads();
         if ((int)threadIdx.x < E) count[threadIdx.x] += had;
-        if (i < end) p.slots[i] = e >= 0 ? (int32_t)rank : -1;
+        if (i0 + kRouteWarps * 32 >= end) break;
+        if (i < end) p.slots[i] = e >= 0 ? (int32_t)number : -1;
+        i0 += kRouteWarps * 32;
     }
     __syncthreads();
-    if (!p.clustered) {
-        for (int e = threadIdx.x; e < E; e += kRouteWarps * 32) p.counts[(int64_t)blockIdx.x * E + e] = count[e];
-        return;
-    }
-    // One cluster: the counts of the CTAs before this one, and of all.
-    if (p.chunks > 1) ptx::cluster_sync_all();
-    uint32_t before = 0;
+    // Every CTA of the cluster gets every CTA's counts.
+    ptx::cluster_wait();
     if ((int)threadIdx.x < E) {
-        uint32_t all = 0;
-        for (int c = 0; c < p.chunks; ++c) {
-            uint32_t n = count[threadIdx.x];
-            if (p.chunks > 1) {
-                const uint32_t from = ptx::map_to_cta(ptx::smem_addr(&count[threadIdx.x]), (uint32_t)c);
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(from) : "memory");
-            }
-            all += n;
-            if (c < (int)blockIdx.x) before += n;
+#pragma unroll
+        for (uint32_t c = 0; c < kRouteCluster; ++c)
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ptx::map_to_cta(ptx::smem_addr(&from[rank][threadIdx.x]), c)), "r"(count[threadIdx.x]) : "memory");
+    }
+    ptx::cluster_sync_all();
+    uint32_t before = 0, all = 0;
+    if ((int)threadIdx.x < E) {
+#pragma unroll
+        for (uint32_t c = 0; c < kRouteCluster; ++c) {
+            all += from[c][threadIdx.x];
+            if (c < rank) before += from[c][threadIdx.x];
         }
-        total[threadIdx.x] = all;
+        count[threadIdx.x] = all;
     }
     __syncthreads();
-    route_offsets(total, first, sums, E);
-    if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= E; e += kRouteWarps * 32) p.offsets[e] = (int32_t)first[e];
-    if ((int)threadIdx.x < E) total[threadIdx.x] = first[threadIdx.x] + before;
-    __syncthreads();
-    for (int64_t i = begin + threadIdx.x; i < end; i += kRouteWarps * 32) {   // (each thread its own numbers)
-        const int e = local ? (int)local_ids[i - begin] : __ldcg(p.ids + i);
-        if (e >= 0) p.slots[i] = __ldcg(p.slots + i) + (int32_t)total[e];
+    const bool only = gridDim.x == kRouteCluster;
+    if (only) {
+        route_offsets(count, first, sums, E);
+        if (blockIdx.x == 0)
+            for (int c = threadIdx.x; c <= E; c += kRouteWarps * 32) p.offsets[c] = (int32_t)first[c];
+    } else if (rank == 0 && (int)threadIdx.x < E) {
+        p.counts[(int64_t)(blockIdx.x / kRouteCluster) * E + threadIdx.x] = all;
     }
-    if (p.chunks > 1) ptx::cluster_sync_all();   // (nobody leaves while its counts may be read)
+    // what comes before this CTA's rows of an expert: in the cluster, or in all
+    if ((int)threadIdx.x < E) from[0][threadIdx.x] = before + (only ? first[threadIdx.x] : 0u);
+    __syncthreads();
+    const int64_t i = i0 + threadIdx.x;
+    if (i < end) p.slots[i] = e >= 0 ? (int32_t)(number + from[0][e]) : -1;
+    for (int64_t r = begin + threadIdx.x; r < i0; r += kRouteWarps * 32) {   // (each thread its own numbers of earlier rounds)
+        const int er = local ? (int)local_ids[r - begin] : __ldcg(p.ids + r);
+        if (er >= 0) p.slots[r] = __ldcg(p.slots + r) + (int32_t)from[0][er];
+    }
 }
 
 __global__ void __launch_bounds__(kRouteWarps * 32)
@@ -399,6 +402,7 @@ route_place_kernel(const RouteParams p) {
     __shared__ uint32_t total[kRouteMaxExperts], before[kRouteMaxExperts], first[kRouteMaxExperts + 1], sums[kRouteWarps];
     ptx::griddep_launch_dependents();
     const int E = p.E, k = p.top_k;
+    const int clusters = p.chunks / kRouteCluster, own = (int)blockIdx.x / kRouteCluster;
     if ((int)threadIdx.x < E) total[threadIdx.x] = before[threadIdx.x] = 0u;
     __syncthreads();
     ptx::griddep_wait();
@@ -407,10 +411,10 @@ route_place_kernel(const RouteParams p) {
     if (part < parts) {
         uint32_t all = 0, earlier = 0;
 #pragma unroll 16
-        for (int c = part; c < p.chunks; c += parts) {
+        for (int c = part; c < clusters; c += parts) {
             const uint32_t n = __ldcg(p.counts + (int64_t)c * E + mine);
             all += n;
-            if (c < (int)blockIdx.x) earlier += n;
+            if (c < own) earlier += n;
         }
         atomicAdd(&total[mine], all);
         atomicAdd(&before[mine], earlier);
@@ -419,7 +423,7 @@ route_place_kernel(const RouteParams p) {
     route_offsets(total, first, sums, E);
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= E; e += kRouteWarps * 32) p.offsets[e] = (int32_t)first[e];
-    const int64_t m0 = (int64_t)blockIdx.x * p.chunk, m1 = min(p.M, m0 + p.chunk);
+    const int64_t m0 = min(p.M, (int64_t)blockIdx.x * p.chunk), m1 = min(p.M, m0 + p.chunk);
     for (int64_t i = m0 * k + threadIdx.x; i < m1 * k; i += kRouteWarps * 32) {
         const int e = __ldcg(p.ids + i);
         if (e >= 0) p.slots[i] = __ldcg(p.slots + i) + (int32_t)(first[e] + before[e]);
