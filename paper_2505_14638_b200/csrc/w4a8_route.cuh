@@ -4,7 +4,7 @@
 // route_choose_kernel: clusters of eight CTAs, a warp per token, V consecutive experts per lane; then a CTA counts its tokens'
 // experts, numbers the rows of each expert in the order of the tokens and tells the other CTAs of the cluster its counts.  Up to
 // 128 tokens that is all: one cluster, one launch.  Above, route_place_kernel follows: every CTA sums the counts of the clusters
-// before its own (at most 36 rows, from L2) and turns the numbers into rows.  No atomics on global memory: the order never varies.
+// before its own (at most 32 rows, from L2) and turns the numbers into rows.  No atomics on global memory: the order never varies.
 //
 // Nothing here is near the bound of its bytes (2 MB of logits: 0.4 us): what counts are launches and the length of the chain of
 // dependent steps of a token -- load, keys, groups, top_k rounds of a warp-wide maximum, weights.  Hence: a key carries its
@@ -28,7 +28,7 @@ namespace w4a8 {
 constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 32, kRouteMaxGroups = 32;
 constexpr int kRouteWarps = 16;      // tokens that a CTA works on at a time
 constexpr int kRouteCluster = 8;
-constexpr int kRouteChunks = 288;    // CTAs at most: two per SM
+constexpr int kRouteChunks = 256;    // CTAs at most: 32 clusters are resident at two CTAs per SM, 36 took a second round
 constexpr int kRouteLocalIds = 2048; // choices of a CTA that are kept in shared memory
 
 struct RouteParams {
