@@ -47,7 +47,8 @@ static bool allow_smem(Kernel kernel, std::atomic<uint64_t>& done) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
     if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1u)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmemMax) != cudaSuccess) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmemMax) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
@@ -92,17 +93,15 @@ static bool make_map(CUtensorMap* m, const void* ptr, uint32_t rank, const cuuin
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+static_assert(sizeof(ExpertTable) <= (size_t)kBlocksTableBytes, "the table's place in shared memory");
+
 template <int TMAX>
-static int launch_blocks(const CUtensorMap& tw, const CUtensorMap& tx, BlocksParams& p, int sms, int64_t tiles, cudaStream_t st) {
+static int launch_blocks(const CUtensorMap& tw, const CUtensorMap& tx, const BlocksParams& p, const BlocksPlan& pl, int sms, int64_t tiles, cudaStream_t st) {
     using Cfg = BlocksCfg<TMAX>;
     static std::atomic<uint64_t> allowed{0};
     if (!allow_smem(linear_blocks_kernel<Cfg>, allowed)) return W4A8_ERR_CUDA;
-    const int fixed = Cfg::fixed_bytes(p.offsets != nullptr, p.cut);
-    p.xslot = (p.tokens + 31) / 32 * 4096;
-    p.stages = (kBlocksSmemMax - fixed) / (16384 + p.xslot);
-    if (p.stages > kBlocksMaxStages) p.stages = kBlocksMaxStages;
-    const int64_t clusters = tiles < sms / p.cut ? tiles : sms / p.cut;
-    return launch(linear_blocks_kernel<Cfg>, (unsigned)(clusters * p.cut), kBlocksThreads, (size_t)(fixed + p.stages * (16384 + p.xslot)), p.cut, st, tw, tx, p);
+    const int64_t most = (int64_t)sms * pl.ctas / pl.cut, clusters = tiles < most ? tiles : most;
+    return launch(linear_blocks_kernel<Cfg>, (unsigned)(clusters * pl.cut), kBlocksThreads, (size_t)pl.smem, pl.cut, st, tw, tx, p);
 }
 
 static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x, int64_t lds, int64_t rows, const int32_t* offsets,
@@ -123,14 +122,15 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     const int sms = sm_count();
     unsigned int* status = status_word_ptr();
     if (sms <= 0 || !status) return W4A8_ERR_CUDA;
-    const BlocksPlan pl = blocks_plan(rows, experts, N, K, sms);
-    const int64_t tiles = NB * (ceil_div(rows, pl.tokens) + (offsets ? experts : 0));   // (with experts: at most)
+    const BlocksPlan pl = blocks_plan(rows, experts, N, K, sms, offsets != nullptr);
+    // (with experts: at most)
+    const int64_t tiles = ceil_div(N, pl.pair ? 256 : pl.channels) * (ceil_div(rows, pl.tokens) + (offsets ? experts : 0));
     if (tiles > INT32_MAX / 2) return W4A8_ERR_BAD_SHAPE;
     CUtensorMap tw, tx;
     {
         const cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)experts};
         const cuuint64_t strides[2] = {(cuuint64_t)ldw, (cuuint64_t)(experts > 1 ? w_stride : N * ldw)};
-        const cuuint32_t box[3] = {128, 128, 1};
+        const cuuint32_t box[3] = {128, pl.pair ? 128u : (cuuint32_t)pl.channels, 1};
         if (!make_map(&tw, w8, 3, dims, strides, box)) return W4A8_ERR_CUDA;
     }
     {
@@ -150,7 +150,6 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     p.N = (int)N;
     p.KB = (int)KB;
     p.NB = (int)NB;
-    p.cut = pl.cut;
     p.tokens = pl.tokens;
     p.out_fp32 = out_dtype == W4A8_OUT_FP32 ? 1 : 0;
     p.status = status;
@@ -160,11 +159,18 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
         const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
         return launch(linear_blocks_pair_kernel, (unsigned)(2 * pairs), kPairBlocksThreads, (size_t)pair_blocks_smem(offsets != nullptr), 2, st, tw, tx, p);
     }
+    p.channels = pl.channels;
+    p.row_tiles = (int)ceil_div(N, pl.channels);
+    p.cut = pl.cut;
+    p.share = pl.share;
+    p.stages = pl.stages;
+    p.xslot = (pl.tokens + 31) / 32 * 4096;
+    p.part_buffers = pl.part_buffers;
     switch (pl.tmax) {
-        case 16: return launch_blocks<16>(tw, tx, p, sms, tiles, st);
-        case 32: return launch_blocks<32>(tw, tx, p, sms, tiles, st);
-        case 64: return launch_blocks<64>(tw, tx, p, sms, tiles, st);
-        default: return launch_blocks<128>(tw, tx, p, sms, tiles, st);
+        case 16: return launch_blocks<16>(tw, tx, p, pl, sms, tiles, st);
+        case 32: return launch_blocks<32>(tw, tx, p, pl, sms, tiles, st);
+        case 64: return launch_blocks<64>(tw, tx, p, pl, sms, tiles, st);
+        default: return launch_blocks<128>(tw, tx, p, pl, sms, tiles, st);
     }
 }
 

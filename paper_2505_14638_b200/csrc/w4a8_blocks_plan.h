@@ -1,59 +1,120 @@
-// How a linear layer with block scales is laid out on the SMs: host code without CUDA, so that it can be tested anywhere.
+// How a linear layer with block scales is laid out on the SMs: host code (and what the kernel shares with it) without CUDA, so that
+// it can be tested anywhere.
 #pragma once
 
 #include <stdint.h>
 
+#ifdef __CUDACC__
+#define W4A8_BOTH __host__ __device__
+#else
+#define W4A8_BOTH
+#endif
+
 namespace w4a8 {
 
-constexpr int kBlocksSmemMax = 232448;
-
-struct BlocksPlan {
-    bool pair;     // CTA pairs: tiles of 256 tokens x 256 channels
-    int tmax;      // tokens that the kernel's registers are laid out for: 16, 32, 64, 128
-    int tokens;    // tokens of a tile at most
-    int cut;       // CTAs that share a tile's K
-};
+constexpr int kBlocksSmemMax = 232448;       // of a block
+constexpr int kBlocksSmemHalf = 115712;      // of two blocks on an SM, each
+constexpr int kBlocksMaxStages = 16, kBlocksBuffers = 4;
+constexpr int kBlocksChunk = 8;              // k-blocks whose activation scales are fetched at a time
+constexpr int kBlocksBars = 2 * kBlocksMaxStages + 2 * kBlocksBuffers + 2 + 2 + 1;
+constexpr int kBlocksTableBytes = 2 * 513 * 4 + 32;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Shared memory of linear_blocks_kernel behind a 1024-byte boundary: the ring, and from where on the rest lies.
+struct BlocksSmem {
+    int bars, scales, table, parts, end;
+};
+W4A8_BOTH inline BlocksSmem blocks_smem(int tmax, int channels, int tokens, int stages, int cut, int share, int part_buffers, bool grouped) {
+    BlocksSmem s;
+    const int ring = stages * (channels * 128 + (tokens + 31) / 32 * 4096);
+    s.bars = ring;
+    s.scales = s.bars + (8 * kBlocksBars + 8 + 15) / 16 * 16;
+    s.table = s.scales + 2 * 2 * kBlocksChunk * tmax * 4;
+    s.parts = s.table + (grouped ? (kBlocksTableBytes + 15) / 16 * 16 : 0);
+    s.end = s.parts + part_buffers * cut * tokens * share * 4;
+    // (an MMA reads 128 rows from where a stage's weights begin, the last stage's too)
+    const int read = ring - (channels * 128 + (tokens + 31) / 32 * 4096) + 16384;
+    if (s.end < read) s.end = read;
+    return s;
+}
+
+struct BlocksPlan {
+    bool pair;         // CTA pairs: tiles of 256 tokens x 256 channels
+    int tmax;          // tokens that the kernel's registers are laid out for: 16, 32, 64, 128
+    int tokens;        // tokens of a tile at most
+    int channels;      // channels of a tile
+    int cut, share;    // CTAs that share a tile's K, and channels that each of them writes
+    int part_buffers;
+    int stages, smem;
+    int ctas;          // per SM
+    int64_t tiles;     // (expected, where there are several experts)
+};
+
+// The ring's depth, and the shared memory, for `rounds` tiles per CTA; false where a plan does not fit.
+inline bool blocks_fit(BlocksPlan* pl, int64_t rounds, bool grouped) {
+    pl->share = (int)(ceil_div(ceil_div(pl->channels, pl->cut), 8) * 8);
+    const int most = pl->ctas == 2 ? kBlocksSmemHalf : kBlocksSmemMax;
+    for (pl->part_buffers = rounds > 1 ? 2 : 1; pl->part_buffers >= 1; --pl->part_buffers)
+        for (pl->stages = kBlocksMaxStages; pl->stages >= 4; --pl->stages) {
+            const BlocksSmem s = blocks_smem(pl->tmax, pl->channels, pl->tokens, pl->stages, pl->cut, pl->share, pl->part_buffers, grouped);
+            pl->smem = 1024 + s.end;
+            if (pl->smem <= most) return true;
+        }
+    return false;
+}
+
 // rows of x8, over `experts` (1: a single layer, whose rows all use it).  The loads of the experts are not known on the host: an
 // expert is expected to have up to four times the average.
-inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t K, int sms) {
-    BlocksPlan pl;
-    const int64_t KB = ceil_div(K, 128), NB = ceil_div(N, 128);
+inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t K, int sms, bool grouped) {
+    BlocksPlan best = {};
+    const int64_t KB = ceil_div(K, 128);
+    best.pair = rows > 128 * experts;
+    if (best.pair) {
+        best.tokens = 256;
+        best.tiles = ceil_div(N, 256) * (ceil_div(rows, 256) + (grouped ? experts : 0));
+        return best;
+    }
     int64_t load = rows;
     if (experts > 1) {
         load = 4 * ceil_div(rows, experts) + 12;
         if (load > rows) load = rows;
     }
-    pl.pair = rows > 128 * experts;
-    if (pl.pair) {
-        pl.tmax = 0;
-        pl.tokens = 256;
-        pl.cut = 1;
-        return pl;
-    }
-    pl.tmax = load <= 16 ? 16 : load <= 32 ? 32 : load <= 64 ? 64 : 128;
-    pl.tokens = load >= 128 ? 128 : (int)ceil_div(load, 16) * 16;
-    int64_t tiles = NB * ceil_div(rows, pl.tokens);
+    const int tmax = load <= 16 ? 16 : load <= 32 ? 32 : load <= 64 ? 64 : 128;
+    const int tokens = load >= 128 ? 128 : (int)ceil_div(load, 16) * 16;
+    int64_t token_tiles = ceil_div(rows, tokens);
     if (experts > 1) {
-        const int64_t full = rows / pl.tokens, with_rows = experts < rows ? experts : rows;
-        tiles = NB * (full > with_rows ? full : with_rows);
+        const int64_t full = rows / tokens, with_rows = experts < rows ? experts : rows;
+        token_tiles = full > with_rows ? full : with_rows;
     }
-    // A CTA's time for a tile: its k-blocks at the SM's share of HBM, and a start and an end; the exchange in a cluster.
-    pl.cut = 1;
-    double best = 1e30;
-    for (int cut = 1; cut <= 8 && cut <= KB; ++cut) {
-        const int64_t clusters = sms / cut;
-        if (clusters < 1) break;
-        const int64_t rounds = ceil_div(tiles, clusters);
-        const double t = (double)rounds * ((double)ceil_div(KB, cut) * 0.35 + (cut > 1 ? 1.0 : 0.3));
-        if (t < best * 0.97) {
-            best = t;
+    // Time in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us): k-blocks, each at least as long as its
+    // round of waits, and a tile's start and end.
+    double least = 1e30;
+    for (int channels = 128; channels >= 32; channels -= 8) {
+        for (int cut = 1; cut <= 8 && cut <= KB; ++cut) {
+            BlocksPlan pl = {};
+            pl.tmax = tmax;
+            pl.tokens = tokens;
+            pl.channels = channels;
             pl.cut = cut;
+            pl.ctas = tmax <= 32 ? 2 : 1;
+            pl.tiles = ceil_div(N, channels) * token_tiles;
+            const int64_t clusters = (int64_t)sms * pl.ctas / cut;
+            if (clusters < 1) break;
+            const int64_t rounds = ceil_div(pl.tiles, clusters);
+            if (!blocks_fit(&pl, grouped ? 2 : rounds, grouped)) continue;
+            const double on_sm = pl.tiles * cut > sms ? pl.ctas : 1;   // CTAs that share an SM's part of HBM
+            double kb = channels / 128.0 * on_sm;
+            const double floor = 0.6 + 0.004 * tokens;
+            if (kb < floor) kb = floor;
+            const double t = (double)rounds * ((double)ceil_div(KB, cut) * kb + 2.0) + (cut > 1 ? 2.0 : 0.0);
+            if (t < least * 0.98) {
+                least = t;
+                best = pl;
+            }
         }
     }
-    return pl;
+    return best;
 }
 
 }  // namespace w4a8

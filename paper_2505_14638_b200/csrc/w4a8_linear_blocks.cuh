@@ -1,22 +1,28 @@
 // FP8 linear layers with a scale per block of 128 (activations: one per token and 128 columns; weights: one per 128 x 128):
 //   y[m][n] = sum_b s_x[m][b] * s_w[n / 128][b] * P_b[m][n],   P_b[m][n] = sum over the 128 columns of block b of x8 * w8,
-// of one layer, or of several experts whose rows lie one behind the other.
+// of one layer, or of several experts whose rows lie one behind the other.  P_b is one k-block's MMAs into a buffer of its own in
+// tensor memory (FP32); warps fetch it and add s_x * s_w times it to sums in registers -- the scales change with every
+// k-block, so the tensor cores cannot go on adding.
 //
-// linear_blocks_kernel: a tile is 128 output channels x up to TMAX tokens.  P_b is one k-block's MMAs into a buffer of its own in
-// tensor memory (FP32); four warps, a thread per channel, fetch it and add s_x * s_w times it to sums in registers -- the scales
-// change with every k-block, so the tensor cores cannot go on adding.  The weights are the A operand (128 rows), the tokens the
-// B operand (N = the tile's tokens rounded up to 16), so that few tokens cost few columns.
+// linear_blocks_kernel (few tokens): a tile is up to 128 output channels x up to TMAX tokens.  The weights are the A operand, the
+// tokens the B operand (N = the tile's tokens rounded up to 16), so that few tokens cost few columns; a thread sums one channel.
 //
-// Few tokens are bound by the weight stream: one stage of the ring is a k-block of weights (16 KB) with its activations, loaded by
-// TMA in the 128-byte swizzle.  Where the tiles do not fill the SMs, the CTAs of a cluster take a part of K each and exchange
-// their sums through distributed shared memory: each adds the parts of its share of the channels, in ascending order of K, so
-// results repeat.  No workspace is needed, so nothing of one call can meet another's.
+// Bound by the weight stream: a stage of the ring is a k-block of weights with its activations, loaded by TMA in the 128-byte
+// swizzle.  The plan (w4a8_blocks_plan.h) takes as many channels per tile as make the tiles come out even over the SMs, and
+// where there are too few, the CTAs of a cluster take a part of K each.  Sums go to the CTA that adds and writes their channels
+// (itself where K is not cut) through distributed shared memory, to be added there in ascending order of K by two warps of
+// their own, while the others are at the next tile: results repeat, no workspace is needed, so nothing of one call can meet
+// another's, and outputs are written in pieces of 16 bytes.
 //
-// Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 idle after the start, 4..7 sums and outputs.
+// A stage's weights may be fewer than the 128 rows that an MMA reads: the other rows are whatever lies behind them, and give sums
+// of channels that nothing looks at.
+//
+// Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 outputs, 4..7 sums.
 #pragma once
 
 #include <cuda_bf16.h>
 
+#include "w4a8_blocks_plan.h"
 #include "w4a8_common.cuh"
 #include "w4a8_ptx.cuh"
 
@@ -24,8 +30,6 @@ namespace w4a8 {
 
 constexpr int kBlocksMaxExperts = 512;
 constexpr int kBlocksThreads = 256;
-constexpr int kBlocksMaxStages = 16, kBlocksBuffers = 4;
-constexpr int kBlocksChunk = 8;    // k-blocks whose activation scales are fetched at a time
 
 struct BlocksParams {
     const float *s_x, *s_w;
@@ -33,10 +37,14 @@ struct BlocksParams {
     void* y;
     int64_t lds, ldy, rows;
     int E, N, KB, NB;         // experts; channels; k-blocks; channel blocks
-    int cut;                  // CTAs (a cluster) that share a tile's K
-    int stages, xslot;        // ring: stages, bytes of a stage's activations (whole boxes of 32 tokens)
-    int tokens;               // tokens of a tile at most
     int out_fp32;
+    int tokens;               // tokens of a tile at most
+    // linear_blocks_kernel
+    int channels, row_tiles;  // channels of a tile (a multiple of 8), tiles of all channels
+    int cut;                  // CTAs (a cluster) that share a tile's K
+    int share;                // channels of a tile that each of them writes
+    int stages, xslot;        // ring: stages, bytes of a stage's activations (whole boxes of 32 tokens)
+    int part_buffers;         // tiles whose sums may be on their way
     unsigned int* status;
 };
 
@@ -44,44 +52,71 @@ struct BlocksParams {
 struct ExpertTable {
     int32_t row[kBlocksMaxExperts + 1];    // first row; row[E] = end of the last
     int32_t tile[kBlocksMaxExperts + 1];   // token tiles of the experts before
+    int32_t sums[8];
 };
 
-// The first warp fills the table.  Offsets are taken into [0, rows] and in ascending order, whatever they hold.
+// All threads of the block (256 of them work) fill the table; a barrier ends it.  Offsets are taken into [0, rows] and in ascending
+// order, whatever they hold.
 __device__ __forceinline__ void fill_expert_table(ExpertTable* t, const int32_t* offsets, int E, int64_t rows, int tokens) {
-    const int lane = threadIdx.x & 31;
+    static_assert(kBlocksMaxExperts == 512, "two experts per thread");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool works = tid < 256;
     const int32_t most = (int32_t)rows;
-    int32_t begin_all = 0, tiles = 0;
-    for (int e0 = 0; e0 <= E; e0 += 32) {
-        const int e = e0 + lane;
-        int32_t r = e <= E ? min(max(__ldg(offsets + e), 0), most) : most;
+    if (works) {
+        int32_t r[3];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int32_t before = __shfl_up_sync(0xFFFFFFFFu, r, o);
-            if (lane >= o) r = max(r, before);
-        }
-        r = max(r, begin_all);
-        begin_all = __shfl_sync(0xFFFFFFFFu, r, 31);
-        if (e <= E) t->row[e] = r;
+        for (int i = 0; i < 3; ++i) r[i] = tid + 256 * i <= E ? __ldg(offsets + tid + 256 * i) : 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (tid + 256 * i <= E) t->row[tid + 256 * i] = min(max(r[i], 0), most);
     }
-    __syncwarp();
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane;
-        const int32_t own = e < E ? (t->row[e + 1] - t->row[e] + tokens - 1) / tokens : 0;
-        int32_t sum = own;
+    __syncthreads();
+    bool descends = false;
+    for (int e = 1 + tid; works && e <= E; e += 256) descends = descends || t->row[e] < t->row[e - 1];
+    if (__syncthreads_or(descends)) {
+        if (warp == 0) {
+            int32_t before_all = 0;
+            for (int e0 = 0; e0 <= E; e0 += 32) {
+                int32_t r = e0 + lane <= E ? t->row[e0 + lane] : most;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int32_t before = __shfl_up_sync(0xFFFFFFFFu, r, o);
+                    if (lane >= o) r = max(r, before);
+                }
+                r = max(r, before_all);
+                before_all = __shfl_sync(0xFFFFFFFFu, r, 31);
+                if (e0 + lane <= E) t->row[e0 + lane] = r;
+            }
+        }
+        __syncthreads();
+    }
+    int32_t own[2] = {0, 0}, sum = 0;
+    if (works) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (2 * tid + i < E) own[i] = (t->row[2 * tid + i + 1] - t->row[2 * tid + i] + tokens - 1) / tokens;
+        sum = own[0] + own[1];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int32_t before = __shfl_up_sync(0xFFFFFFFFu, sum, o);
             if (lane >= o) sum += before;
         }
-        if (e < E) t->tile[e] = tiles + sum - own;
-        tiles += __shfl_sync(0xFFFFFFFFu, sum, 31);
+        if (lane == 31) t->sums[warp] = sum;
     }
-    if (lane == 0) t->tile[E] = tiles;
+    __syncthreads();
+    if (works) {
+#pragma unroll
+        for (int w = 0; w < 8; ++w) sum += w < warp ? t->sums[w] : 0;
+        if (2 * tid < E) t->tile[2 * tid] = sum - own[0] - own[1];
+        if (2 * tid + 1 < E) t->tile[2 * tid + 1] = sum - own[1];
+        if (tid == 255) t->tile[E] = sum;
+    }
+    __syncthreads();
 }
 
-// A tile: expert, first channel block, rows.
+// A tile: expert, rows, and where its channels begin.
 struct BlocksTile {
-    int e, nb, count;   // expert, channel block, tokens
+    int e, nb, count;   // expert; first channel block (pairs) or first channel; tokens
     int64_t row;        // first row
 };
 // The rows of token tile j.
@@ -105,16 +140,16 @@ __device__ __forceinline__ BlocksTile blocks_rows(const BlocksParams& p, const E
     b.count = min(p.tokens, t->row[lo + 1] - t->row[lo] - at);
     return b;
 }
-// The channel blocks of a token tile follow one another.
+// The channel tiles of a token tile follow one another.
 __device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const ExpertTable* t, int i) {
-    const int j = i / p.NB;
+    const int j = i / p.row_tiles;
     BlocksTile b = blocks_rows(p, t, j);
-    b.nb = i - j * p.NB;
+    b.nb = (i - j * p.row_tiles) * p.channels;
     return b;
 }
 
-// Arrival on a barrier of a CTA of the cluster that also announces this thread's writes to that CTA's shared memory, and the wait
-// that goes with it.
+// Arrival on a barrier of a CTA of the cluster that also announces what this thread has written to that CTA's shared memory, or
+// read from its own.
 __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
@@ -127,20 +162,40 @@ struct BlocksCfg {
     static constexpr int TMAX = TMAX_;
     static constexpr int kAccCols = TMAX_ < 32 ? 32 : TMAX_;
     static constexpr int kTmemCols = kBlocksBuffers * kAccCols;
-    static constexpr int kBarBytes = 8 * (2 * kBlocksMaxStages + 2 * kBlocksBuffers + 2 + 1) + 16;
-    // (behind the ring) barriers, scales [2][chunk][TMAX], experts, parts of other CTAs [cut][TMAX][channels of a share]
-    static constexpr int kScaleBytes = 2 * kBlocksChunk * TMAX_ * 4;
-    __host__ __device__ static constexpr int table_bytes(bool grouped) { return grouped ? (int)sizeof(ExpertTable) : 0; }
-    __host__ __device__ static constexpr int part_bytes(int cut) { return cut > 1 ? cut * ((128 + cut - 1) / cut) * TMAX_ * 4 : 0; }
-    static constexpr int kSmemMax = 232448;
-    __host__ __device__ static constexpr int fixed_bytes(bool grouped, int cut) {
-        return 1024 + ((kBarBytes + 15) / 16 * 16) + kScaleBytes + (table_bytes(grouped) + 15) / 16 * 16 + part_bytes(cut);
-    }
+    static constexpr int kCtas = TMAX_ <= 32 ? 2 : 1;   // per SM
 };
 
+// Eight channels of a token.
+__device__ __forceinline__ void store8(const BlocksParams& p, int64_t at, int have, bool wide, const float (&v)[8]) {
+    if (p.out_fp32) {
+        float* y = static_cast<float*>(p.y) + at;
+        if (wide) {
+            reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) y[i] = v[i];
+        }
+    } else {
+        __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + at;
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        if (wide) {
+            *reinterpret_cast<uint4*>(y) = make_uint4(*reinterpret_cast<uint32_t*>(&h[0]), *reinterpret_cast<uint32_t*>(&h[1]),
+                                                      *reinterpret_cast<uint32_t*>(&h[2]), *reinterpret_cast<uint32_t*>(&h[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) y[i] = i & 1 ? h[i >> 1].y : h[i >> 1].x;
+        }
+    }
+}
+
 template <class Cfg>
-__global__ void __launch_bounds__(kBlocksThreads, 1)
-linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
+__global__ void __launch_bounds__(kBlocksThreads, Cfg::kCtas)
+linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x channels x 1, 128B swizzle
                      const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 32, 128B swizzle
                      const BlocksParams p) {
     constexpr int TMAX = Cfg::TMAX, NBUF = kBlocksBuffers;
@@ -148,31 +203,25 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     const uint32_t base = (raw_addr + 1023u) & ~1023u;
     uint8_t* sm = smem_raw + (base - raw_addr);
-    const uint32_t stage_bytes = 16384u + (uint32_t)p.xslot;
-    uint32_t off = (uint32_t)p.stages * stage_bytes;
-    const uint32_t bars = base + off;
+    const BlocksSmem lay = blocks_smem(TMAX, p.channels, p.tokens, p.stages, p.cut, p.share, p.part_buffers, p.offsets != nullptr);
+    const uint32_t wslot = (uint32_t)p.channels * 128u, stage_bytes = wslot + (uint32_t)p.xslot;
+    const uint32_t bars = base + (uint32_t)lay.bars;
     const uint32_t bar_full = bars, bar_free = bar_full + 8u * kBlocksMaxStages;
     const uint32_t bar_acc = bar_free + 8u * kBlocksMaxStages, bar_acc_free = bar_acc + 8u * NBUF;
-    const uint32_t bar_parts = bar_acc_free + 8u * NBUF, bar_parts_free = bar_parts + 8u, bar_drain = bar_parts + 16u;
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + off + 8u * (2 * kBlocksMaxStages + 2 * NBUF + 3));
+    const uint32_t bar_parts = bar_acc_free + 8u * NBUF, bar_parts_free = bar_parts + 16u, bar_drain = bar_parts_free + 16u;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + lay.bars + 8 * kBlocksBars);
     volatile uint32_t* abort_flag = tmem_slot + 1;
-    off += (uint32_t)(Cfg::kBarBytes + 15) / 16u * 16u;
-    float* scales = reinterpret_cast<float*>(sm + off);   // [2][chunk][TMAX]
-    off += (uint32_t)Cfg::kScaleBytes;
-    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + off);
-    off += (uint32_t)(Cfg::table_bytes(p.offsets != nullptr) + 15) / 16u * 16u;
-    float* parts = reinterpret_cast<float*>(sm + off);    // [cut][TMAX][share]
-    const uint32_t parts_addr = base + off;
+    float* scales = reinterpret_cast<float*>(sm + lay.scales);   // [2 buffers][2 channel blocks][k-block][TMAX]
+    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + lay.table);
+    const uint32_t parts_addr = base + (uint32_t)lay.parts;      // [buffer][CTA][token][channel of the share]
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cut = p.cut, rank = cut > 1 ? (int)ptx::cluster_ctarank() : 0;
-    const int share = (128 + cut - 1) / cut;
+    const int cut = p.cut, rank = cut > 1 ? (int)ptx::cluster_ctarank() : 0, share = p.share;
     const int kb0 = rank * p.KB / cut, KB = (rank + 1) * p.KB / cut - kb0;
+    const int first = (int)blockIdx.x / cut, step = (int)gridDim.x / cut;
+    const bool grouped = p.offsets != nullptr;
 
-    if (warp == 1) {
-        ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), Cfg::kTmemCols);
-        ptx::tmem_relinquish();
-    } else if (warp == 2) {
+    if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < p.stages; ++i) {
                 ptx::mbar_init(bar_full + 8u * i, 1);
@@ -182,27 +231,40 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                 ptx::mbar_init(bar_acc + 8u * i, 1);
                 ptx::mbar_init(bar_acc_free + 8u * i, 4);
             }
-            ptx::mbar_init(bar_parts, (uint32_t)cut * 4u);
-            ptx::mbar_init(bar_parts_free, (uint32_t)cut);
+            for (int i = 0; i < 2; ++i) {
+                ptx::mbar_init(bar_parts + 8u * i, (uint32_t)cut * 4u);
+                ptx::mbar_init(bar_parts_free + 8u * i, (uint32_t)cut);
+            }
             ptx::mbar_init(bar_drain, 1);
             *abort_flag = 0u;
             ptx::fence_mbar_init();
         }
-    } else if (warp == 3 && lane == 0) {
+        __syncwarp();
+    } else if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), Cfg::kTmemCols);
+        ptx::tmem_relinquish();
+    } else if (warp == 2 && lane == 0) {
         ptx::prefetch_tensormap(&tmap_w);
         ptx::prefetch_tensormap(&tmap_x);
+        // The weights of the first tile are brought to L2 while earlier kernels finish.  (A prefetch reads nothing that they may still
+        // write: what they write reaches L2.)
+        if (!grouped && first < p.row_tiles)
+            for (int b = 0; b < KB; ++b) ptx::tma_prefetch_3d(&tmap_w, (kb0 + b) * 128, first * p.channels, 0);
     }
+    if (cut > 1) ptx::cluster_arrive_relaxed();   // (behind the barriers' set-up; waited for ahead of the first access to another CTA)
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    if (warp == 0 && p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
     ptx::tc_fence_before_sync();
-    __syncthreads();
-    if (cut > 1) ptx::cluster_sync_all();   // (barriers of the peers are there before anything arrives on them)
+    if (grouped) {
+        fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
+    } else if (warp == 0) {   // (the loads need none of the others)
+        asm volatile("bar.arrive 2, %0;" ::"n"(kBlocksThreads) : "memory");
+    } else {
+        asm volatile("bar.sync 2, %0;" ::"n"(kBlocksThreads) : "memory");
+    }
     ptx::tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;
-    const int token_tiles = p.offsets != nullptr ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
-    const int tiles = token_tiles * p.NB;
-    const int first = (int)blockIdx.x / cut, step = (int)gridDim.x / cut;
+    const int token_tiles = grouped ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
+    const int tiles = token_tiles * p.row_tiles;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ loads (whole warp, one lane issues)
@@ -212,16 +274,16 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
         for (int i = first; i < tiles && ok; i += step) {
             const BlocksTile t = blocks_tile(p, table, i);
             const int boxes = (t.count + 31) >> 5;
-            const uint32_t bytes = 16384u + (uint32_t)boxes * 4096u;
+            const uint32_t bytes = wslot + (uint32_t)boxes * 4096u;
             for (int b = 0; b < KB; ++b) {
                 if (issued >= p.stages) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
                 if (!ok) break;
                 const uint32_t full = bar_full + 8u * r.idx, dst = base + (uint32_t)r.idx * stage_bytes;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(full, bytes);
-                    ptx::tma_load_3d(dst, &tmap_w, (kb0 + b) * 128, t.nb * 128, t.e, full);
+                    ptx::tma_load_3d(dst, &tmap_w, (kb0 + b) * 128, t.nb, t.e, full);
                     for (int q = 0; q < boxes; ++q)
-                        ptx::tma_load_2d(dst + 16384u + (uint32_t)q * 4096u, &tmap_x, (kb0 + b) * 128, (int)t.row + 32 * q, full);
+                        ptx::tma_load_2d(dst + wslot + (uint32_t)q * 4096u, &tmap_x, (kb0 + b) * 128, (int)t.row + 32 * q, full);
                 }
                 r.advance(p.stages);
                 ++issued;
@@ -235,8 +297,10 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                 }
         }
         __syncwarp();
+        if (cut > 1) ptx::cluster_wait();
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMAs (whole warp, one lane issues)
+        const uint32_t tmem = *tmem_slot;
         bool ok = true;
         ptx::Ring r, a;
         int made = 0;
@@ -249,11 +313,11 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t w = base + (uint32_t)r.idx * stage_bytes;
-                const uint32_t a_lo = ptx::umma_desc_lo(w), b_lo = ptx::umma_desc_lo(w + 16384u);
+                const uint32_t a_lo = ptx::umma_desc_lo(w), b_lo = ptx::umma_desc_lo(w + wslot);
                 if (ptx::elect_one()) {
                     ptx::umma_f8_kblock(tmem + (uint32_t)(a.idx * Cfg::kAccCols), a_lo, b_lo, idesc, 0u);
-                    ptx::umma_commit(bar_free + 8u * r.idx);
                     ptx::umma_commit(bar_acc + 8u * a.idx);
+                    ptx::umma_commit(bar_free + 8u * r.idx);
                 }
                 r.advance(p.stages);
                 a.advance(NBUF);
@@ -267,119 +331,138 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
             }
         }
         __syncwarp();
-    } else if (warp >= 4) {
-        // ------------------------------------------------------------------ sums and outputs: thread = channel of the tile
-        const int tid = (int)threadIdx.x - 128;   // channel within the tile; token in the scale fetches
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        bool ok = true;
-        ptx::Ring a;
-        uint32_t exchanged = 0;
-        int c = 0;
-        // (after a wait that gave up these warps still walk all tiles, without waiting or writing: they meet at a barrier)
-        for (int i = first; i < tiles; i += step) {
-            const BlocksTile t = blocks_tile(p, table, i);
-            const float* sw_row = p.s_w + ((int64_t)t.e * p.NB + t.nb) * p.KB + kb0;
-            const float* sx_row = p.s_x + (t.row + tid) * p.lds + kb0;
-            const bool token = tid < t.count;
-            unsigned long long acc[TMAX / 2];
+        if (cut > 1) ptx::cluster_wait();
+    } else {
+        // The CTAs' parts of this CTA's channels of a tile, added in ascending order of K and written: eight channels of a token at a
+        // time, by `n` threads.  Returns whether the parts came.
+        const bool wide = ((p.ldy * (p.out_fp32 ? 4 : 2)) & 15) == 0;   // rows of y 16-byte aligned (y itself is)
+        const int part_floats = cut * p.tokens * share;
+        auto write_tile = [&](const BlocksTile& t, int at, uint32_t phase, int me, int n) -> bool {
+            if (!ptx::mbar_wait_warp(bar_parts + 8u * at, phase, abort_flag, p.status)) return false;
+            if (cut > 1) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+            const int n0 = t.nb + rank * share, have = min(min(share, p.channels - rank * share), p.N - n0), groups = (have + 7) >> 3;
+            const uint32_t from = parts_addr + (uint32_t)(at * part_floats * 4);
+            for (int u = me; u < groups * t.count; u += n) {
+                const int tok = u / groups, c = (u - tok * groups) * 8;
+                float v[8] = {};
+                for (int q = 0; q < cut; ++q) {
+                    const uint32_t a = from + (uint32_t)(((q * p.tokens + tok) * share + c) * 4);
+                    float w[8];
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]) : "r"(a) : "memory");
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(w[4]), "=f"(w[5]), "=f"(w[6]), "=f"(w[7]) : "r"(a + 16u) : "memory");
 #pragma unroll
-            for (int j = 0; j < TMAX / 2; ++j) acc[j] = 0ull;
-            float next[kBlocksChunk];   // this thread's token's scales of the next chunk of k-blocks
-#pragma unroll
-            for (int j = 0; j < kBlocksChunk; ++j) next[j] = token && j < KB ? __ldg(sx_row + j) * __ldg(sw_row + j) : 0.0f;
-            for (int b0 = 0; b0 < KB; b0 += kBlocksChunk, c ^= 1) {
-                float* cur = scales + c * kBlocksChunk * TMAX;
-                if (tid < TMAX) {
-#pragma unroll
-                    for (int j = 0; j < kBlocksChunk; ++j) cur[j * TMAX + tid] = next[j];
+                    for (int k = 0; k < 8; ++k) v[k] = q == 0 ? w[k] : v[k] + w[k];
                 }
-                // (two buffers: a warp writes a chunk's scales only when all have finished with the chunk before the last)
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-#pragma unroll
-                for (int j = 0; j < kBlocksChunk; ++j) {
-                    const int b = b0 + kBlocksChunk + j;
-                    next[j] = token && b < KB ? __ldg(sx_row + b) * __ldg(sw_row + b) : 0.0f;
+                store8(p, (t.row + tok) * p.ldy + n0 + c, have - c, wide && have - c >= 8, v);
+            }
+            return true;
+        };
+        const int last_tile = first < tiles ? first + (tiles - 1 - first) / step * step : -1;
+        if (warp < 4) {
+            // -------------------------------------------------------------- outputs
+            if (cut > 1) ptx::cluster_wait();
+            int use = 0;
+            bool ok = true;
+            // (after a wait that gave up these two warps still walk all tiles, without waiting or writing: they meet at a barrier)
+            for (int i = first; i < tiles; i += step, ++use) {
+                const int at = p.part_buffers == 2 ? use & 1 : 0, times = p.part_buffers == 2 ? use >> 1 : use;
+                // (the last tile's are written by the other four warps as well)
+                ok = ok && write_tile(blocks_tile(p, table, i), at, (uint32_t)times & 1u, (int)threadIdx.x - 64, i == last_tile ? 192 : 64);
+                if (i + (int64_t)p.part_buffers * step < tiles) {   // the buffer's next tile may come
+                    asm volatile("bar.sync 3, 64;" ::: "memory");
+                    if (ok && warp == 2 && lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts_free + 8u * at, (uint32_t)lane));
                 }
-                const int end = min(kBlocksChunk, KB - b0);
-                for (int j = 0; j < end; ++j) {
-                    ok = ok && ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
-                    if (!ok) break;   // (warp-uniform)
-                    ptx::tc_fence_after_sync();
-                    const ulonglong2* f = reinterpret_cast<const ulonglong2*>(cur + j * TMAX);
-                    const uint32_t src = lanes + (uint32_t)(a.idx * Cfg::kAccCols);
+            }
+        } else {
+            // -------------------------------------------------------------- sums: thread = channel of the tile
+            const int tid = (int)threadIdx.x - 128;   // channel within the tile; token in the scale fetches
+            const uint32_t lanes = *tmem_slot + ((uint32_t)((warp & 3) * 32) << 16);
+            if (cut > 1) ptx::cluster_wait();
+            bool ok = true;
+            ptx::Ring a;
+            int use = 0, c = 0;
+            const bool channel = tid < p.channels, any = (warp & 3) * 32 < p.channels;
+            // (after a wait that gave up these warps still walk all tiles, without waiting or writing: they meet at a barrier)
+            for (int i = first; i < tiles; i += step, ++use) {
+                const BlocksTile t = blocks_tile(p, table, i);
+                const int blk = t.nb >> 7, mine = (min(t.nb + tid, p.N - 1) >> 7) - blk;   // channel block: the tile's first, or the next
+                const float* sw_row = p.s_w + ((int64_t)t.e * p.NB + blk) * p.KB + kb0;
+                // (lanes 0..7 fetch the scales of eight k-blocks of the first block, 8..15 of the next)
+                const float* sw_lane = sw_row + (lane >= 8 && blk + 1 < p.NB ? p.KB : 0) + (lane & 7);
+                const float* sx_row = p.s_x + (t.row + tid) * p.lds + kb0;
+                const bool token = tid < t.count;
+                unsigned long long acc[TMAX / 2];
 #pragma unroll
-                    for (int q = 0; q < TMAX / 16; ++q) {
-                        if (q * 16 >= t.count) break;
-                        uint32_t v[16];
-                        ptx::tmem_ld_32x32b_x16(src + (uint32_t)(q * 16), v);
-                        ptx::tmem_ld_wait_for(v);
+                for (int j = 0; j < TMAX / 2; ++j) acc[j] = 0ull;
+                float next[kBlocksChunk];   // this thread's token's scales of the next chunk of k-blocks
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            const ulonglong2 s = f[q * 4 + h];   // the scales of four tokens
-                            acc[q * 8 + 2 * h] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h]), __uint_as_float(v[4 * h + 1])), s.x, acc[q * 8 + 2 * h]);
-                            acc[q * 8 + 2 * h + 1] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h + 2]), __uint_as_float(v[4 * h + 3])), s.y, acc[q * 8 + 2 * h + 1]);
+                for (int j = 0; j < kBlocksChunk; ++j) next[j] = token && j < KB ? __ldg(sx_row + j) : 0.0f;
+                float next_w = lane < 16 && (lane & 7) < KB ? __ldg(sw_lane) : 0.0f;
+                for (int b0 = 0; b0 < KB; b0 += kBlocksChunk, c ^= 1) {
+                    float* cur = scales + c * 2 * kBlocksChunk * TMAX;
+#pragma unroll
+                    for (int j = 0; j < kBlocksChunk; ++j) {
+                        const float w0 = __shfl_sync(0xFFFFFFFFu, next_w, j), w1 = __shfl_sync(0xFFFFFFFFu, next_w, 8 + j);
+                        if (tid < TMAX) {
+                            cur[j * TMAX + tid] = next[j] * w0;
+                            cur[(kBlocksChunk + j) * TMAX + tid] = next[j] * w1;
                         }
                     }
-                    ptx::tc_fence_before_sync();
+                    // (two buffers: a warp writes a chunk's scales only when all have finished with the chunk before the last)
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < kBlocksChunk; ++j) {
+                        const int b = b0 + kBlocksChunk + j;
+                        next[j] = token && b < KB ? __ldg(sx_row + b) : 0.0f;
+                    }
+                    next_w = lane < 16 && b0 + kBlocksChunk + (lane & 7) < KB ? __ldg(sw_lane + b0 + kBlocksChunk) : 0.0f;
+                    const int end = min(kBlocksChunk, KB - b0);
+                    for (int j = 0; j < end; ++j) {
+                        ok = ok && ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
+                        if (!ok) break;   // (warp-uniform)
+                        ptx::tc_fence_after_sync();
+                        const ulonglong2* f = reinterpret_cast<const ulonglong2*>(cur + (mine * kBlocksChunk + j) * TMAX);
+                        const uint32_t src = lanes + (uint32_t)(a.idx * Cfg::kAccCols);
+#pragma unroll
+                        for (int q = 0; q < TMAX / 16; ++q) {
+                            if (q * 16 >= t.count || !any) break;
+                            uint32_t v[16];
+                            ptx::tmem_ld_32x32b_x16(src + (uint32_t)(q * 16), v);
+                            ptx::tmem_ld_wait_for(v);
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+                                const ulonglong2 s = f[q * 4 + h];   // the scales of four tokens
+                                acc[q * 8 + 2 * h] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h]), __uint_as_float(v[4 * h + 1])), s.x, acc[q * 8 + 2 * h]);
+                                acc[q * 8 + 2 * h + 1] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h + 2]), __uint_as_float(v[4 * h + 3])), s.y, acc[q * 8 + 2 * h + 1]);
+                            }
+                        }
+                        ptx::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(bar_acc_free + 8u * a.idx);
+                        a.advance(NBUF);
+                    }
+                }
+                // The sums of this thread's channel go to the CTA that writes it, once that has read those of an earlier tile.
+                const int at = p.part_buffers == 2 ? use & 1 : 0, times = p.part_buffers == 2 ? use >> 1 : use;
+                if (times > 0) ok = ok && ptx::mbar_wait_warp(bar_parts_free + 8u * at, (uint32_t)(times - 1) & 1u, abort_flag, p.status);
+                if (ok) {
+                    if (channel) {
+                        const int owner = tid / share;
+                        const uint32_t to = ptx::map_to_cta(parts_addr, (uint32_t)owner) + (uint32_t)((at * part_floats + rank * p.tokens * share + tid - owner * share) * 4);
+#pragma unroll
+                        for (int j = 0; j < TMAX / 2; ++j) {
+                            float lo, hi;
+                            unpack_f32x2(acc[j], lo, hi);
+                            if (2 * j < t.count) st_cluster_f32(to + (uint32_t)(2 * j * share * 4), lo);
+                            if (2 * j + 1 < t.count) st_cluster_f32(to + (uint32_t)((2 * j + 1) * share * 4), hi);
+                        }
+                    }
+                    if (cut > 1) asm volatile("fence.acq_rel.cluster;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(bar_acc_free + 8u * a.idx);
-                    a.advance(NBUF);
+                    if (lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts + 8u * at, (uint32_t)lane));
+                    if (i == last_tile) ok = write_tile(t, at, (uint32_t)times & 1u, tid + 64, 192);
                 }
             }
-            if (cut == 1) {
-                const int n = t.nb * 128 + tid;
-                if (ok && n < p.N) {
-#pragma unroll
-                    for (int j = 0; j < TMAX / 2; ++j) {
-                        float lo, hi;
-                        unpack_f32x2(acc[j], lo, hi);
-                        const int64_t at = (t.row + 2 * j) * p.ldy + n;
-                        if (p.out_fp32) {
-                            if (2 * j < t.count) static_cast<float*>(p.y)[at] = lo;
-                            if (2 * j + 1 < t.count) static_cast<float*>(p.y)[at + p.ldy] = hi;
-                        } else {
-                            if (2 * j < t.count) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(lo);
-                            if (2 * j + 1 < t.count) static_cast<__nv_bfloat16*>(p.y)[at + p.ldy] = __float2bfloat16_rn(hi);
-                        }
-                    }
-                }
-                continue;
-            }
-            // The parts of this thread's channel go to the CTA that adds them, once that has read those of the tile before.
-            if (exchanged > 0) ok = ok && ptx::mbar_wait_warp(bar_parts_free, (exchanged - 1u) & 1u, abort_flag, p.status);
-            if (ok) {
-                const int owner = tid / share;
-                const uint32_t to = ptx::map_to_cta(parts_addr, (uint32_t)owner) + (uint32_t)((rank * TMAX * share + tid - owner * share) * 4);
-#pragma unroll
-                for (int j = 0; j < TMAX / 2; ++j) {
-                    float lo, hi;
-                    unpack_f32x2(acc[j], lo, hi);
-                    if (2 * j < t.count) st_cluster_f32(to + (uint32_t)(2 * j * share * 4), lo);
-                    if (2 * j + 1 < t.count) st_cluster_f32(to + (uint32_t)((2 * j + 1) * share * 4), hi);
-                }
-                asm volatile("fence.acq_rel.cluster;" ::: "memory");
-                __syncwarp();
-                if (lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts, (uint32_t)lane));
-                ok = ptx::mbar_wait_warp(bar_parts, exchanged & 1u, abort_flag, p.status);
-                asm volatile("fence.acq_rel.cluster;" ::: "memory");
-            }
-            if (ok) {
-                const int n0 = t.nb * 128 + rank * share, have = min(share, 128 - rank * share);
-                for (int e = tid; e < t.count * share; e += 128) {
-                    const int tok = e / share, c = e - tok * share;
-                    if (c >= have || n0 + c >= p.N) continue;
-                    float s = 0.0f;
-                    for (int q = 0; q < cut; ++q) s += parts[(q * TMAX + tok) * share + c];
-                    const int64_t at = (t.row + tok) * p.ldy + n0 + c;
-                    if (p.out_fp32)
-                        static_cast<float*>(p.y)[at] = s;
-                    else
-                        static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(s);
-                }
-            }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (warp == 4 && lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts_free, (uint32_t)lane));
-            ++exchanged;
         }
     }
 
@@ -387,9 +470,21 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     __syncthreads();
     if (warp == 1) {
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc(tmem, Cfg::kTmemCols);
+        ptx::tmem_dealloc(*tmem_slot, Cfg::kTmemCols);
     }
-    if (cut > 1) ptx::cluster_sync_all();   // (no CTA goes away while another writes to its shared memory or arrives on its barriers)
+    if (cut > 1) {
+        // Closing barrier: no CTA goes away while another writes to its shared memory or arrives on its barriers.  It orders execution
+        // only: parts have been waited for by those that write them, and a buffer's release is sent only where it will be.
+        const bool gave_up = *abort_flag != 0u;
+        if (gave_up) ptx::cluster_arrive();
+        else ptx::cluster_arrive_relaxed();
+        ptx::cluster_wait();
+        if (gave_up) {   // (not all of it then: late arrivals have 2 ms)
+            const uint64_t t0 = ptx::globaltimer_ns();
+            while (ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 1000) {
+            }
+        }
+    }
 }
 
 // ---- many tokens: CTA pairs ----------------------------------------------------------------------------------------------------
@@ -471,9 +566,9 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
     }
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    if (warp == 8 && p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
     ptx::tc_fence_before_sync();
-    __syncthreads();
+    if (p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
+    else __syncthreads();
     ptx::cluster_sync_all();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
