@@ -101,7 +101,7 @@ static int launch_blocks(const CUtensorMap& tw, const CUtensorMap& tx, const Blo
     static std::atomic<uint64_t> allowed{0};
     if (!allow_smem(linear_blocks_kernel<Cfg>, allowed)) return W4A8_ERR_CUDA;
     const int64_t most = (int64_t)sms * pl.ctas / pl.cut, clusters = tiles < most ? tiles : most;
-    return launch(linear_blocks_kernel<Cfg>, (unsigned)(clusters * pl.cut), kBlocksThreads, (size_t)pl.smem, pl.cut, st, tw, tx, p);
+    return launch(linear_blocks_kernel<Cfg>, (unsigned)(clusters * pl.cut), Cfg::kThreads, (size_t)pl.smem, pl.cut, st, tw, tx, p);
 }
 
 static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x, int64_t lds, int64_t rows, const int32_t* offsets,

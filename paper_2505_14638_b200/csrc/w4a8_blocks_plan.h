@@ -44,7 +44,7 @@ struct BlocksPlan {
     int tmax;          // tokens that the kernel's registers are laid out for: 16, 32, 64, 128
     int tokens;        // tokens of a tile at most
     int channels;      // channels of a tile
-    int cut, share;    // CTAs that share a tile's K, and channels that each of them writes
+    int cut, share;    // CTAs that share a tile's K, and channels that each of them writes, at most
     int part_buffers;
     int stages, smem;
     int ctas;          // per SM
@@ -53,7 +53,8 @@ struct BlocksPlan {
 
 // The ring's depth, and the shared memory, for `rounds` tiles per CTA; false where a plan does not fit.
 inline bool blocks_fit(BlocksPlan* pl, int64_t rounds, bool grouped) {
-    pl->share = (int)(ceil_div(ceil_div(pl->channels, pl->cut), 8) * 8);
+    if (pl->channels < 8 * pl->cut) return false;   // (at least eight channels each)
+    pl->share = (int)(ceil_div(pl->channels / 8, pl->cut) * 8);
     const int most = pl->ctas == 2 ? kBlocksSmemHalf : kBlocksSmemMax;
     for (pl->part_buffers = rounds > 1 ? 2 : 1; pl->part_buffers >= 1; --pl->part_buffers)
         for (pl->stages = kBlocksMaxStages; pl->stages >= 4; --pl->stages) {
@@ -87,33 +88,44 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
         const int64_t full = rows / tokens, with_rows = experts < rows ? experts : rows;
         token_tiles = full > with_rows ? full : with_rows;
     }
-    // Time in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us): k-blocks, each at least as long as its
-    // round of waits, and a tile's start and end.
+    // Time in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us): a tile's k-blocks, each at least as long as
+    // its round of waits, and its start and end.
+    const int ctas = tmax <= 32 ? 2 : 1;
+    const double floor = 0.55 + 0.004 * tokens;
     double least = 1e30;
-    for (int channels = 128; channels >= 32; channels -= 8) {
-        for (int cut = 1; cut <= 8 && cut <= KB; ++cut) {
-            BlocksPlan pl = {};
-            pl.tmax = tmax;
-            pl.tokens = tokens;
-            pl.channels = channels;
-            pl.cut = cut;
-            pl.ctas = tmax <= 32 ? 2 : 1;
-            pl.tiles = ceil_div(N, channels) * token_tiles;
-            const int64_t clusters = (int64_t)sms * pl.ctas / cut;
-            if (clusters < 1) break;
-            const int64_t rounds = ceil_div(pl.tiles, clusters);
-            if (!blocks_fit(&pl, grouped ? 2 : rounds, grouped)) continue;
-            const double on_sm = pl.tiles * cut > sms ? pl.ctas : 1;   // CTAs that share an SM's part of HBM
-            double kb = channels / 128.0 * on_sm;
-            const double floor = 0.6 + 0.004 * tokens;
-            if (kb < floor) kb = floor;
-            const double t = (double)rounds * ((double)ceil_div(KB, cut) * kb + 2.0) + (cut > 1 ? 2.0 : 0.0);
-            if (t < least * 0.98) {
-                least = t;
-                best = pl;
-            }
+    auto consider = [&](int channels, int cut) {   // whether it fits
+        BlocksPlan pl = {};
+        pl.tmax = tmax;
+        pl.tokens = tokens;
+        pl.channels = channels;
+        pl.cut = cut;
+        pl.ctas = ctas;
+        pl.tiles = ceil_div(N, channels) * token_tiles;
+        const int64_t rounds = ceil_div(pl.tiles, (int64_t)sms * ctas / cut);
+        if (!blocks_fit(&pl, grouped ? 2 : rounds, grouped)) return false;
+        double t;
+        if (cut == 1) {
+            const double kb = channels / 128.0 * (pl.tiles > sms ? ctas : 1);
+            t = (double)rounds * ((double)KB * (kb > floor ? kb : floor) + 2.0);
+        } else {
+            const double stream = (double)pl.tiles * (double)KB / sms, walk = (double)ceil_div(KB, cut) * floor;
+            t = (stream > walk ? stream : walk) + 4.5;
         }
-    }
+        if (t < least) {
+            least = t;
+            best = pl;
+        }
+        return true;
+    };
+    for (int channels = 128; channels >= 64; channels -= 8) consider(channels, 1);
+    // K is cut where that fills the SMs in one round, as far as it does: a tenth of the places is left, since a cluster's lie in one
+    // group of SMs, and the groups' sizes are no multiples of it.  Measured, us, not cut / cut: (1, 6144, 4096) 14.8 / 9.2,
+    // (16, 4096, 14336) 41 / 14.8, (64, 4096, 4096) 18.2 / 10.9.
+    const int64_t tiles = ceil_div(N, 128) * token_tiles;
+    int64_t cut = (int64_t)(0.9 * sms * ctas) / tiles;
+    if (cut > 8) cut = 8;
+    if (cut > KB / 3) cut = KB / 3;
+    while (cut >= 2 && !consider(128, (int)cut)) --cut;
     return best;
 }
 

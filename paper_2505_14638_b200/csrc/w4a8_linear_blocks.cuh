@@ -17,7 +17,8 @@
 // A stage's weights may be fewer than the 128 rows that an MMA reads: the other rows are whatever lies behind them, and give sums
 // of channels that nothing looks at.
 //
-// Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 outputs, 4..7 sums.
+// Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 outputs, then one group of four that adds, or two above 32 tokens
+// (each half of the tokens: with one, 80 tokens were bound by it, 780 cycles a k-block).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -29,7 +30,6 @@
 namespace w4a8 {
 
 constexpr int kBlocksMaxExperts = 512;
-constexpr int kBlocksThreads = 256;
 
 struct BlocksParams {
     const float *s_x, *s_w;
@@ -42,7 +42,7 @@ struct BlocksParams {
     // linear_blocks_kernel
     int channels, row_tiles;  // channels of a tile (a multiple of 8), tiles of all channels
     int cut;                  // CTAs (a cluster) that share a tile's K
-    int share;                // channels of a tile that each of them writes
+    int share;                // channels of a tile that each of them writes, at most
     int stages, xslot;        // ring: stages, bytes of a stage's activations (whole boxes of 32 tokens)
     int part_buffers;         // tiles whose sums may be on their way
     unsigned int* status;
@@ -153,8 +153,19 @@ __device__ __forceinline__ BlocksTile blocks_tile(const BlocksParams& p, const E
 __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+// A value into the shared memory of a CTA of the cluster; its four bytes complete on a barrier of that CTA.
+__device__ __forceinline__ void st_async_f32(uint32_t addr, float v, uint32_t cluster_bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(addr), "r"(__float_as_uint(v)), "r"(cluster_bar)
+                 : "memory");
+}
+// Behind a wait: what other CTAs of the cluster have sent is visible too.
+__device__ __forceinline__ void acquire_cluster(uint32_t bar, uint32_t parity) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t"
+        "}\n" ::"r"(bar), "r"(parity)
+        : "memory");
 }
 
 template <int TMAX_>
@@ -163,6 +174,9 @@ struct BlocksCfg {
     static constexpr int kAccCols = TMAX_ < 32 ? 32 : TMAX_;
     static constexpr int kTmemCols = kBlocksBuffers * kAccCols;
     static constexpr int kCtas = TMAX_ <= 32 ? 2 : 1;   // per SM
+    static constexpr int G = TMAX_ <= 32 ? 1 : 2;       // groups of warps that add
+    static constexpr int TG = TMAX_ / G;                // tokens of each
+    static constexpr int kThreads = 128 + 128 * G;
 };
 
 // Eight channels of a token.
@@ -194,11 +208,11 @@ __device__ __forceinline__ void store8(const BlocksParams& p, int64_t at, int ha
 }
 
 template <class Cfg>
-__global__ void __launch_bounds__(kBlocksThreads, Cfg::kCtas)
+__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtas)
 linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x channels x 1, 128B swizzle
                      const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 32, 128B swizzle
                      const BlocksParams p) {
-    constexpr int TMAX = Cfg::TMAX, NBUF = kBlocksBuffers;
+    constexpr int TMAX = Cfg::TMAX, NBUF = kBlocksBuffers, G = Cfg::G, TG = Cfg::TG;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     const uint32_t base = (raw_addr + 1023u) & ~1023u;
@@ -218,6 +232,9 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cut = p.cut, rank = cut > 1 ? (int)ptx::cluster_ctarank() : 0, share = p.share;
     const int kb0 = rank * p.KB / cut, KB = (rank + 1) * p.KB / cut - kb0;
+    // A tile's channels are dealt out to the CTAs that write them in units of eight, at least one each: a CTA without any would have
+    // nothing to wait for, and run ahead of those that send to it.
+    const int units = p.channels >> 3, mine0 = rank * units / cut * 8, mine_n = (rank + 1) * units / cut * 8 - mine0;
     const int first = (int)blockIdx.x / cut, step = (int)gridDim.x / cut;
     const bool grouped = p.offsets != nullptr;
 
@@ -229,10 +246,10 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
             }
             for (int i = 0; i < NBUF; ++i) {
                 ptx::mbar_init(bar_acc + 8u * i, 1);
-                ptx::mbar_init(bar_acc_free + 8u * i, 4);
+                ptx::mbar_init(bar_acc_free + 8u * i, 4 * G);
             }
             for (int i = 0; i < 2; ++i) {
-                ptx::mbar_init(bar_parts + 8u * i, (uint32_t)cut * 4u);
+                ptx::mbar_init(bar_parts + 8u * i, cut > 1 ? 1u : 4u * G);   // (bytes of all CTAs; or this one's warps)
                 ptx::mbar_init(bar_parts_free + 8u * i, (uint32_t)cut);
             }
             ptx::mbar_init(bar_drain, 1);
@@ -246,10 +263,6 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     } else if (warp == 2 && lane == 0) {
         ptx::prefetch_tensormap(&tmap_w);
         ptx::prefetch_tensormap(&tmap_x);
-        // The weights of the first tile are brought to L2 while earlier kernels finish.  (A prefetch reads nothing that they may still
-        // write: what they write reaches L2.)
-        if (!grouped && first < p.row_tiles)
-            for (int b = 0; b < KB; ++b) ptx::tma_prefetch_3d(&tmap_w, (kb0 + b) * 128, first * p.channels, 0);
     }
     if (cut > 1) ptx::cluster_arrive_relaxed();   // (behind the barriers' set-up; waited for ahead of the first access to another CTA)
     ptx::griddep_launch_dependents();
@@ -258,9 +271,9 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     if (grouped) {
         fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
     } else if (warp == 0) {   // (the loads need none of the others)
-        asm volatile("bar.arrive 2, %0;" ::"n"(kBlocksThreads) : "memory");
+        asm volatile("bar.arrive 2, %0;" ::"n"(Cfg::kThreads) : "memory");
     } else {
-        asm volatile("bar.sync 2, %0;" ::"n"(kBlocksThreads) : "memory");
+        asm volatile("bar.sync 2, %0;" ::"n"(Cfg::kThreads) : "memory");
     }
     ptx::tc_fence_after_sync();
     const int token_tiles = grouped ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
@@ -339,8 +352,8 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
         const int part_floats = cut * p.tokens * share;
         auto write_tile = [&](const BlocksTile& t, int at, uint32_t phase, int me, int n) -> bool {
             if (!ptx::mbar_wait_warp(bar_parts + 8u * at, phase, abort_flag, p.status)) return false;
-            if (cut > 1) asm volatile("fence.acq_rel.cluster;" ::: "memory");
-            const int n0 = t.nb + rank * share, have = min(min(share, p.channels - rank * share), p.N - n0), groups = (have + 7) >> 3;
+            if (cut > 1) acquire_cluster(bar_parts + 8u * at, phase);
+            const int n0 = t.nb + mine0, have = min(mine_n, p.N - n0), groups = (have + 7) >> 3;
             const uint32_t from = parts_addr + (uint32_t)(at * part_floats * 4);
             for (int u = me; u < groups * t.count; u += n) {
                 const int tok = u / groups, c = (u - tok * groups) * 8;
@@ -366,22 +379,26 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
             // (after a wait that gave up these two warps still walk all tiles, without waiting or writing: they meet at a barrier)
             for (int i = first; i < tiles; i += step, ++use) {
                 const int at = p.part_buffers == 2 ? use & 1 : 0, times = p.part_buffers == 2 ? use >> 1 : use;
-                // (the last tile's are written by the other four warps as well)
-                ok = ok && write_tile(blocks_tile(p, table, i), at, (uint32_t)times & 1u, (int)threadIdx.x - 64, i == last_tile ? 192 : 64);
+                const BlocksTile t = blocks_tile(p, table, i);
+                if (cut > 1 && warp == 2 && lane == 0)
+                    ptx::mbar_arrive_expect_tx(bar_parts + 8u * at, (uint32_t)(cut * t.count * mine_n * 4));
+                // (the last tile's are written by the warps that add as well)
+                ok = ok && write_tile(t, at, (uint32_t)times & 1u, (int)threadIdx.x - 64, i == last_tile ? 64 + 128 * G : 64);
                 if (i + (int64_t)p.part_buffers * step < tiles) {   // the buffer's next tile may come
                     asm volatile("bar.sync 3, 64;" ::: "memory");
                     if (ok && warp == 2 && lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts_free + 8u * at, (uint32_t)lane));
                 }
             }
         } else {
-            // -------------------------------------------------------------- sums: thread = channel of the tile
-            const int tid = (int)threadIdx.x - 128;   // channel within the tile; token in the scale fetches
+            // -------------------------------------------------------------- sums: thread = channel of the tile, and a group's tokens
+            const int all = (int)threadIdx.x - 128, tid = all & 127, g0 = all >> 7 ? TG : 0;   // (all: token in the scale fetches)
             const uint32_t lanes = *tmem_slot + ((uint32_t)((warp & 3) * 32) << 16);
             if (cut > 1) ptx::cluster_wait();
             bool ok = true;
             ptx::Ring a;
             int use = 0, c = 0;
             const bool channel = tid < p.channels, any = (warp & 3) * 32 < p.channels;
+            const int owner = channel ? (((tid >> 3) + 1) * cut - 1) / units : 0, column = tid - owner * units / cut * 8;   // who writes this channel
             // (after a wait that gave up these warps still walk all tiles, without waiting or writing: they meet at a barrier)
             for (int i = first; i < tiles; i += step, ++use) {
                 const BlocksTile t = blocks_tile(p, table, i);
@@ -389,11 +406,12 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                 const float* sw_row = p.s_w + ((int64_t)t.e * p.NB + blk) * p.KB + kb0;
                 // (lanes 0..7 fetch the scales of eight k-blocks of the first block, 8..15 of the next)
                 const float* sw_lane = sw_row + (lane >= 8 && blk + 1 < p.NB ? p.KB : 0) + (lane & 7);
-                const float* sx_row = p.s_x + (t.row + tid) * p.lds + kb0;
-                const bool token = tid < t.count;
-                unsigned long long acc[TMAX / 2];
+                const float* sx_row = p.s_x + (t.row + all) * p.lds + kb0;
+                const bool token = all < t.count;
+                const int mine_count = t.count - g0;   // tokens of this group and later ones
+                unsigned long long acc[TG / 2];
 #pragma unroll
-                for (int j = 0; j < TMAX / 2; ++j) acc[j] = 0ull;
+                for (int j = 0; j < TG / 2; ++j) acc[j] = 0ull;
                 float next[kBlocksChunk];   // this thread's token's scales of the next chunk of k-blocks
 #pragma unroll
                 for (int j = 0; j < kBlocksChunk; ++j) next[j] = token && j < KB ? __ldg(sx_row + j) : 0.0f;
@@ -403,13 +421,13 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
 #pragma unroll
                     for (int j = 0; j < kBlocksChunk; ++j) {
                         const float w0 = __shfl_sync(0xFFFFFFFFu, next_w, j), w1 = __shfl_sync(0xFFFFFFFFu, next_w, 8 + j);
-                        if (tid < TMAX) {
-                            cur[j * TMAX + tid] = next[j] * w0;
-                            cur[(kBlocksChunk + j) * TMAX + tid] = next[j] * w1;
+                        if (all < TMAX) {
+                            cur[j * TMAX + all] = next[j] * w0;
+                            cur[(kBlocksChunk + j) * TMAX + all] = next[j] * w1;
                         }
                     }
                     // (two buffers: a warp writes a chunk's scales only when all have finished with the chunk before the last)
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
 #pragma unroll
                     for (int j = 0; j < kBlocksChunk; ++j) {
                         const int b = b0 + kBlocksChunk + j;
@@ -421,19 +439,23 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                         ok = ok && ptx::mbar_wait_warp(bar_acc + 8u * a.idx, a.phase, abort_flag, p.status);
                         if (!ok) break;   // (warp-uniform)
                         ptx::tc_fence_after_sync();
-                        const ulonglong2* f = reinterpret_cast<const ulonglong2*>(cur + (mine * kBlocksChunk + j) * TMAX);
-                        const uint32_t src = lanes + (uint32_t)(a.idx * Cfg::kAccCols);
+                        const ulonglong2* f = reinterpret_cast<const ulonglong2*>(cur + (mine * kBlocksChunk + j) * TMAX + g0);
+                        const uint32_t src = lanes + (uint32_t)(a.idx * Cfg::kAccCols + g0);
+                        if (any && mine_count > 0) {
+                            uint32_t v[2][16];   // sixteen tokens are on their way while those before are added
+                            ptx::tmem_ld_32x32b_x16(src, v[0]);
 #pragma unroll
-                        for (int q = 0; q < TMAX / 16; ++q) {
-                            if (q * 16 >= t.count || !any) break;
-                            uint32_t v[16];
-                            ptx::tmem_ld_32x32b_x16(src + (uint32_t)(q * 16), v);
-                            ptx::tmem_ld_wait_for(v);
+                            for (int q = 0; q < TG / 16; ++q) {
+                                if (q * 16 >= mine_count) break;
+                                ptx::tmem_ld_wait_for(v[q & 1]);
+                                if (q + 1 < TG / 16 && (q + 1) * 16 < mine_count) ptx::tmem_ld_32x32b_x16(src + (uint32_t)(q * 16 + 16), v[(q + 1) & 1]);
 #pragma unroll
-                            for (int h = 0; h < 4; ++h) {
-                                const ulonglong2 s = f[q * 4 + h];   // the scales of four tokens
-                                acc[q * 8 + 2 * h] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h]), __uint_as_float(v[4 * h + 1])), s.x, acc[q * 8 + 2 * h]);
-                                acc[q * 8 + 2 * h + 1] = fma_f32x2(pack_f32x2(__uint_as_float(v[4 * h + 2]), __uint_as_float(v[4 * h + 3])), s.y, acc[q * 8 + 2 * h + 1]);
+                                for (int h = 0; h < 4; ++h) {
+                                    const ulonglong2 s = f[q * 4 + h];   // the scales of four tokens
+                                    const uint32_t* x = &v[q & 1][4 * h];
+                                    acc[q * 8 + 2 * h] = fma_f32x2(pack_f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), s.x, acc[q * 8 + 2 * h]);
+                                    acc[q * 8 + 2 * h + 1] = fma_f32x2(pack_f32x2(__uint_as_float(x[2]), __uint_as_float(x[3])), s.y, acc[q * 8 + 2 * h + 1]);
+                                }
                             }
                         }
                         ptx::tc_fence_before_sync();
@@ -446,21 +468,33 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
                 const int at = p.part_buffers == 2 ? use & 1 : 0, times = p.part_buffers == 2 ? use >> 1 : use;
                 if (times > 0) ok = ok && ptx::mbar_wait_warp(bar_parts_free + 8u * at, (uint32_t)(times - 1) & 1u, abort_flag, p.status);
                 if (ok) {
-                    if (channel) {
-                        const int owner = tid / share;
-                        const uint32_t to = ptx::map_to_cta(parts_addr, (uint32_t)owner) + (uint32_t)((at * part_floats + rank * p.tokens * share + tid - owner * share) * 4);
+                    const uint32_t off = (uint32_t)((at * part_floats + (rank * p.tokens + g0) * share + column) * 4);
+                    if (cut > 1) {   // (their bytes complete on the owner's barrier)
+                        if (channel) {
+                            const uint32_t to = ptx::map_to_cta(parts_addr, (uint32_t)owner) + off, bar = ptx::map_to_cta(bar_parts + 8u * at, (uint32_t)owner);
 #pragma unroll
-                        for (int j = 0; j < TMAX / 2; ++j) {
-                            float lo, hi;
-                            unpack_f32x2(acc[j], lo, hi);
-                            if (2 * j < t.count) st_cluster_f32(to + (uint32_t)(2 * j * share * 4), lo);
-                            if (2 * j + 1 < t.count) st_cluster_f32(to + (uint32_t)((2 * j + 1) * share * 4), hi);
+                            for (int j = 0; j < TG / 2; ++j) {
+                                float lo, hi;
+                                unpack_f32x2(acc[j], lo, hi);
+                                if (2 * j < mine_count) st_async_f32(to + (uint32_t)(2 * j * share * 4), lo, bar);
+                                if (2 * j + 1 < mine_count) st_async_f32(to + (uint32_t)((2 * j + 1) * share * 4), hi, bar);
+                            }
                         }
+                    } else {
+                        if (channel) {
+                            const uint32_t to = parts_addr + off;
+#pragma unroll
+                            for (int j = 0; j < TG / 2; ++j) {
+                                float lo, hi;
+                                unpack_f32x2(acc[j], lo, hi);
+                                if (2 * j < mine_count) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (uint32_t)(2 * j * share * 4)), "f"(lo) : "memory");
+                                if (2 * j + 1 < mine_count) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (uint32_t)((2 * j + 1) * share * 4)), "f"(hi) : "memory");
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(bar_parts + 8u * at);
                     }
-                    if (cut > 1) asm volatile("fence.acq_rel.cluster;" ::: "memory");
-                    __syncwarp();
-                    if (lane < cut) mbar_arrive_release_cluster(ptx::map_to_cta(bar_parts + 8u * at, (uint32_t)lane));
-                    if (i == last_tile) ok = write_tile(t, at, (uint32_t)times & 1u, tid + 64, 192);
+                    if (i == last_tile) ok = write_tile(t, at, (uint32_t)times & 1u, all + 64, 64 + 128 * G);
                 }
             }
         }
@@ -472,17 +506,14 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(*tmem_slot, Cfg::kTmemCols);
     }
-    if (cut > 1) {
-        // Closing barrier: no CTA goes away while another writes to its shared memory or arrives on its barriers.  It orders execution
-        // only: parts have been waited for by those that write them, and a buffer's release is sent only where it will be.
-        const bool gave_up = *abort_flag != 0u;
-        if (gave_up) ptx::cluster_arrive();
-        else ptx::cluster_arrive_relaxed();
+    // What is sent to another CTA is waited for there (parts by those that write them; a buffer's release is sent only where its
+    // next use will wait), so a CTA leaves when it is done -- but for one whose wait gave up: it stays until all others are done
+    // or have given up too, and 2 ms more for what may be on its way.
+    if (cut > 1 && *abort_flag != 0u) {
+        ptx::cluster_arrive();
         ptx::cluster_wait();
-        if (gave_up) {   // (not all of it then: late arrivals have 2 ms)
-            const uint64_t t0 = ptx::globaltimer_ns();
-            while (ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 1000) {
-            }
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 1000) {
         }
     }
 }

@@ -228,6 +228,24 @@ def test_experts(counts, N, K):
         out.check()
 
 
+@pytest.mark.parametrize("N,K", [(512, 1664), (384, 2048), (400, 2064), (256, 1040)])
+@pytest.mark.parametrize("counts", [[129, 129, 129, 121, 1, 1, 1, 1], [1] * 7 + [505], [64] * 8, [0, 300, 0, 0, 212, 0, 0, 0]])
+def test_more_tiles_than_expected_where_k_is_cut(counts, N, K):
+    # few channels, so that clusters share K, and experts with more rows than the plan expects: clusters with several tiles
+    rows = sum(counts)
+    g = gen(N + K + counts[0])
+    x8, s_x = random_rows(g, rows, K)
+    w8, s_w = random_weights(g, (8, N, K))
+    out = _out(rows, N, FP32)
+    for _ in range(3):
+        binding.linear_fp8_experts(x8, s_x, _offsets(counts), w8, s_w, out_dtype=binding.OUT_FP32, out=out.t)
+    _clean()
+    y, mag = _experts_ref(x8, s_x, counts, w8, s_w)
+    off = (out.t.double() - y).abs() - linear_tolerance(mag, K, FP32, y)
+    assert bool((off <= 0).all()), float(off.max())
+    out.check()
+
+
 def test_experts_agree_with_single_layers_and_take_strides():
     counts, N, K = [40, 0, 9, 200], 400, 656
     g = gen(12)
