@@ -496,8 +496,8 @@ int w4a8_forward_host(const void* x_host_bf16, int64_t M, const uint8_t* weights
  *   amax = max |x| over the block;  s_x = max(amax, 2^-100) / 448 (fp32 division; 1 when the block is all zero);
  *   X8 = nearest_E4M3( x * (448 / max(amax, 2^-100)) )  -- one fp32 multiply, as w4a8_quantize_act.
  * input_kind W4A8_CHAIN_INPUT_SILU_MUL: x_bf16 holds gate (K columns) and up (K columns behind them), x = silu(gate) * up in
- * FP32 -- not rounded to BF16 in between as in w4a8_silu_mul_quantize.  NaN stays NaN; a block with an infinity has s_x = inf
- * and NaN in its place.
+ * FP32, within 2^-20 -- not rounded to BF16 in between as in w4a8_silu_mul_quantize; gates below -87 count as silu = 0, infinite
+ * ones as NaN.  NaN stays NaN; a block with an infinity has s_x = inf and NaN in its place.
  * slots (int32 [M][top_k], contiguous; NULL with top_k = 0): token m's row is written to the rows slots[m][0..top_k) of x8 and
  * s_x, as w4a8_route_experts gives them; entries outside [0, rows) are skipped, rows that no entry names are left as they were
  * (an entry must not be there twice).  NULL: token m is row m, rows >= M, and rows behind M are left as they were.

@@ -84,8 +84,10 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
     const int tmax = load <= 16 ? 16 : load <= 32 ? 32 : load <= 64 ? 64 : 128;
     const int tokens = load >= 128 ? 128 : (int)ceil_div(load, 16) * 16;
     int64_t token_tiles = ceil_div(rows, tokens);
-    if (experts > 1) {
-        const int64_t full = rows / tokens, with_rows = experts < rows ? experts : rows;
+    if (experts > 1) {   // as many experts as have rows when each row goes to any of them
+        double without = 1.0;
+        for (int64_t r = 0; r < rows && without > 1e-3; ++r) without *= 1.0 - 1.0 / (double)experts;
+        const int64_t full = rows / tokens, with_rows = (int64_t)((double)experts * (1.0 - without) + 0.99);
         token_tiles = full > with_rows ? full : with_rows;
     }
     // Time in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us): a tile's k-blocks, each at least as long as
@@ -101,15 +103,17 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
         pl.cut = cut;
         pl.ctas = ctas;
         pl.tiles = ceil_div(N, channels) * token_tiles;
-        const int64_t rounds = ceil_div(pl.tiles, (int64_t)sms * ctas / cut);
-        if (!blocks_fit(&pl, grouped ? 2 : rounds, grouped)) return false;
+        const int64_t places = (int64_t)sms * ctas / cut;
+        // (tiles of experts are not that many for certain: a last round that may be empty or full counts half)
+        const double rounds = pl.tiles <= places ? 1.0 : grouped ? (double)pl.tiles / places + 0.5 : (double)ceil_div(pl.tiles, places);
+        if (!blocks_fit(&pl, grouped ? 2 : (int64_t)rounds, grouped)) return false;
         double t;
         if (cut == 1) {
             const double kb = channels / 128.0 * (pl.tiles > sms ? ctas : 1);
-            t = (double)rounds * ((double)KB * (kb > floor ? kb : floor) + 2.0);
+            t = rounds * ((double)KB * (kb > floor ? kb : floor) + 2.0);
         } else {
             const double stream = (double)pl.tiles * (double)KB / sms, walk = (double)ceil_div(KB, cut) * floor;
-            t = (stream > walk ? stream : walk) + 4.5;
+            t = (stream > walk ? stream : walk) + 3.5;
         }
         if (t < least) {
             least = t;
@@ -124,7 +128,7 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
     const int64_t tiles = ceil_div(N, 128) * token_tiles;
     int64_t cut = (int64_t)(0.9 * sms * ctas) / tiles;
     if (cut > 8) cut = 8;
-    if (cut > KB / 3) cut = KB / 3;
+    if (cut > KB / 2) cut = KB / 2;
     while (cut >= 2 && !consider(128, (int)cut)) --cut;
     return best;
 }
