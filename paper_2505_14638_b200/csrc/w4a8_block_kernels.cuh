@@ -61,31 +61,50 @@ quantize_blocks_kernel(const uint16_t* __restrict__ x, int M, int K, int64_t ldx
     const int warps = gridDim.x * (blockDim.x >> 5), p0 = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const int row_step = warps / per_row, piece_step = warps - row_step * per_row;
     int64_t m = p0 / per_row;
-    for (int piece = p0 - (int)m * per_row; m < M; m += row_step, piece += piece_step) {
-        if (piece >= per_row) {
-            piece -= per_row;
-            if (++m >= M) break;
+    int piece = p0 - (int)m * per_row;
+    // The next piece's values are on their way while this one's are worked on (the gated kind: 59.5 us without).
+    uint4 ahead[GATED ? 4 : 2];
+    auto fetch = [&]() {
+        const int col = piece * 512 + lane * 16;
+        if (m < M && col < K) {
+            const uint4* src = reinterpret_cast<const uint4*>(x + m * ldx + col);
+            ahead[0] = __ldg(src);
+            ahead[1] = __ldg(src + 1);
+            if constexpr (GATED) {
+                const uint4* up = reinterpret_cast<const uint4*>(x + m * ldx + K + col);
+                ahead[2] = __ldg(up);
+                ahead[3] = __ldg(up + 1);
+            }
         }
+    };
+    fetch();
+    while (m < M) {
+        const int64_t row = m;
         const int col = piece * 512 + lane * 16;
         const bool have = col < K;
+        uint4 now[GATED ? 4 : 2];
+#pragma unroll
+        for (int i = 0; i < (GATED ? 4 : 2); ++i) now[i] = ahead[i];
+        m += row_step;
+        piece += piece_step;
+        if (piece >= per_row) {
+            piece -= per_row;
+            ++m;
+        }
+        fetch();
         float v[16];
         if (have) {
-            const uint4* src = reinterpret_cast<const uint4*>(x + m * ldx + col);
-            const uint4 a = __ldg(src), b = __ldg(src + 1);
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const uint32_t w[8] = {now[0].x, now[0].y, now[0].z, now[0].w, now[1].x, now[1].y, now[1].z, now[1].w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[2 * i] = __uint_as_float(w[i] << 16);
                 v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
             }
             if constexpr (GATED) {
-                const uint4* up = reinterpret_cast<const uint4*>(x + m * ldx + K + col);
-                const uint4 c = __ldg(up), d = __ldg(up + 1);
-                const uint32_t u[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+                const uint32_t u[8] = {now[2].x, now[2].y, now[2].z, now[2].w, now[3].x, now[3].y, now[3].z, now[3].w};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 8; ++i)
                     unpack_f32x2(silu_mul(v[2 * i], v[2 * i + 1], __uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u)), v[2 * i], v[2 * i + 1]);
-                }
             }
         } else {
 #pragma unroll
@@ -107,11 +126,11 @@ quantize_blocks_kernel(const uint16_t* __restrict__ x, int M, int K, int64_t ldx
         q.w = cvt_e4m3x4(v[12], v[13], v[14], v[15]);
         if (!have) continue;   // (no warp-wide step follows)
         if (top_k == 0) {
-            *reinterpret_cast<uint4*>(x8 + m * ldx8 + col) = q;
-            if ((lane & 7) == 0) s_x[m * lds + (col >> 7)] = s;
+            *reinterpret_cast<uint4*>(x8 + row * ldx8 + col) = q;
+            if ((lane & 7) == 0) s_x[row * lds + (col >> 7)] = s;
         } else {
             for (int j = 0; j < top_k; ++j) {
-                const int64_t r = __ldg(slots + m * top_k + j);
+                const int64_t r = __ldg(slots + row * top_k + j);
                 if (r < 0 || r >= rows) continue;
                 *reinterpret_cast<uint4*>(x8 + r * ldx8 + col) = q;
                 if ((lane & 7) == 0) s_x[r * lds + (col >> 7)] = s;
