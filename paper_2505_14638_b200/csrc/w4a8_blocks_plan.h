@@ -2,6 +2,7 @@
 // it can be tested anywhere.
 #pragma once
 
+#include <math.h>
 #include <stdint.h>
 
 #ifdef __CUDACC__
@@ -57,44 +58,51 @@ inline bool blocks_fit(BlocksPlan* pl, int64_t rounds, bool grouped) {
     pl->share = (int)(ceil_div(pl->channels / 8, pl->cut) * 8);
     const int most = pl->ctas == 2 ? kBlocksSmemHalf : kBlocksSmemMax;
     for (pl->part_buffers = rounds > 1 ? 2 : 1; pl->part_buffers >= 1; --pl->part_buffers)
-        for (pl->stages = kBlocksMaxStages; pl->stages >= 4; --pl->stages) {
-            const BlocksSmem s = blocks_smem(pl->tmax, pl->channels, pl->tokens, pl->stages, pl->cut, pl->share, pl->part_buffers, grouped);
-            pl->smem = 1024 + s.end;
+    {
+        const int stage = pl->channels * 128 + (pl->tokens + 31) / 32 * 4096;
+        const int fixed = 1024 + blocks_smem(pl->tmax, pl->channels, pl->tokens, 4, pl->cut, pl->share, pl->part_buffers, grouped).end - 4 * stage;
+        pl->stages = (most - fixed) / stage;   // (at most one too many or too few: the end of a short ring may be further off)
+        if (pl->stages > kBlocksMaxStages) pl->stages = kBlocksMaxStages;
+        for (; pl->stages >= 4; --pl->stages) {
+            pl->smem = 1024 + blocks_smem(pl->tmax, pl->channels, pl->tokens, pl->stages, pl->cut, pl->share, pl->part_buffers, grouped).end;
             if (pl->smem <= most) return true;
         }
+    }
     return false;
 }
 
-// rows of x8, over `experts` (1: a single layer, whose rows all use it).  The loads of the experts are not known on the host: an
-// expert is expected to have up to four times the average.
+// rows of x8, over `experts` (1: a single layer, whose rows all use it).  The loads of the experts are not known on the host: the plan
+// takes each row to go to any of them, and an expert to have up to four times the average.
+//
+// Costs are in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us), without what every launch takes.
+// Measured, us, tiles of up to 128 tokens / pairs: (256, 4096, 4096) 15.4 / 22.4, (512, 1024, 4096) 11.3 / 21.6, (256, 14336, 4096)
+// 37.5 / 24.8, (1024, 4096, 4096) 37.3 / 24.0; 64 experts of (4096, 2048) with 64, 128, 256 rows each 128 / 148, 195 / 163, 355 / 221.
 inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t K, int sms, bool grouped) {
-    BlocksPlan best = {};
     const int64_t KB = ceil_div(K, 128);
-    best.pair = rows > 128 * experts;
-    if (best.pair) {
-        best.tokens = 256;
-        best.tiles = ceil_div(N, 256) * (ceil_div(rows, 256) + (grouped ? experts : 0));
-        return best;
-    }
-    int64_t load = rows;
+    int64_t with_rows = 1, load = rows;
     if (experts > 1) {
+        with_rows = (int64_t)((double)experts * -expm1((double)rows * log1p(-1.0 / (double)experts)) + 0.99);
+        if (with_rows < 1) with_rows = 1;
         load = 4 * ceil_div(rows, experts) + 12;
         if (load > rows) load = rows;
     }
     const int tmax = load <= 16 ? 16 : load <= 32 ? 32 : load <= 64 ? 64 : 128;
-    const int tokens = load >= 128 ? 128 : (int)ceil_div(load, 16) * 16;
-    int64_t token_tiles = ceil_div(rows, tokens);
-    if (experts > 1) {   // as many experts as have rows when each row goes to any of them
-        double without = 1.0;
-        for (int64_t r = 0; r < rows && without > 1e-3; ++r) without *= 1.0 - 1.0 / (double)experts;
-        const int64_t full = rows / tokens, with_rows = (int64_t)((double)experts * (1.0 - without) + 0.99);
-        token_tiles = full > with_rows ? full : with_rows;
-    }
-    // Time in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us): a tile's k-blocks, each at least as long as
-    // its round of waits, and its start and end.
-    const int ctas = tmax <= 32 ? 2 : 1;
-    const double floor = 0.55 + 0.004 * tokens;
+    // (a layer's tokens are dealt out evenly)
+    const int tokens = (int)ceil_div(experts > 1 ? (load < 128 ? load : 128) : ceil_div(rows, ceil_div(rows, 128)), 16) * 16;
+    auto token_tiles = [&](int per) -> int64_t {
+        if (experts == 1) return ceil_div(rows, per);
+        const int64_t n = rows / per + with_rows / 2;   // (half a tile of each expert is empty)
+        return n > with_rows ? n : with_rows;
+    };
+    // (tiles of experts are not that many for certain: a last round that may be empty or full counts half)
+    auto rounds_of = [&](int64_t tiles, int64_t places) -> double {
+        return tiles <= places ? 1.0 : grouped ? (double)tiles / (double)places + 0.5 : (double)ceil_div(tiles, places);
+    };
+
+    BlocksPlan best = {};
     double least = 1e30;
+    const int ctas = tmax <= 32 ? 2 : 1;
+    const double floor = 0.55 + 0.0055 * tokens;   // a k-block's round of waits and additions
     auto consider = [&](int channels, int cut) {   // whether it fits
         BlocksPlan pl = {};
         pl.tmax = tmax;
@@ -102,10 +110,8 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
         pl.channels = channels;
         pl.cut = cut;
         pl.ctas = ctas;
-        pl.tiles = ceil_div(N, channels) * token_tiles;
-        const int64_t places = (int64_t)sms * ctas / cut;
-        // (tiles of experts are not that many for certain: a last round that may be empty or full counts half)
-        const double rounds = pl.tiles <= places ? 1.0 : grouped ? (double)pl.tiles / places + 0.5 : (double)ceil_div(pl.tiles, places);
+        pl.tiles = ceil_div(N, channels) * token_tiles(tokens);
+        const double rounds = rounds_of(pl.tiles, (int64_t)sms * ctas / cut);
         if (!blocks_fit(&pl, grouped ? 2 : (int64_t)rounds, grouped)) return false;
         double t;
         if (cut == 1) {
@@ -123,13 +129,21 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
     };
     for (int channels = 128; channels >= 64; channels -= 8) consider(channels, 1);
     // K is cut where that fills the SMs in one round, as far as it does: a tenth of the places is left, since a cluster's lie in one
-    // group of SMs, and the groups' sizes are no multiples of it.  Measured, us, not cut / cut: (1, 6144, 4096) 14.8 / 9.2,
-    // (16, 4096, 14336) 41 / 14.8, (64, 4096, 4096) 18.2 / 10.9.
-    const int64_t tiles = ceil_div(N, 128) * token_tiles;
-    int64_t cut = (int64_t)(0.9 * sms * ctas) / tiles;
+    // group of SMs, and the groups' sizes are no multiples of it.  Measured, us, not cut / cut: (1, 6144, 4096) 13.8 / 8.3, (16, 4096,
+    // 14336) 39.5 / 14.7, (64, 4096, 4096) 15.4 / 9.4.
+    int64_t cut = (int64_t)(0.9 * sms * ctas) / (ceil_div(N, 128) * token_tiles(tokens));
     if (cut > 8) cut = 8;
     if (cut > KB / 2) cut = KB / 2;
     while (cut >= 2 && !consider(128, (int)cut)) --cut;
+    if (tmax == 128 && rows > 128) {
+        const int64_t tiles = ceil_div(N, 256) * token_tiles(256);
+        if (rounds_of(tiles, sms / 2) * ((double)KB * 1.23 + 4.0) < least) {
+            best = {};
+            best.pair = true;
+            best.tokens = 256;
+            best.tiles = tiles;
+        }
+    }
     return best;
 }
 

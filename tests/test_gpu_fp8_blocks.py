@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from blocks_ref import (E4M3, activation, blocks, gen, linear64, linear_tolerance, quantize_fp32, random_rows, random_weights)
+from blocks_shapes import EXPERTS_FEW, EXPERTS_MANY, EXPERTS_MANY_LAYERS, FEW, MANY
 from gpu_utils import Guarded
 from paper_2505_14638_b200 import binding
 
@@ -120,8 +121,7 @@ def test_strides_of_the_quantization():
 
 
 # ------------------------------------------------------------------------------ one layer
-SHAPES = [(1, 16, 16), (1, 128, 128), (1, 6144, 4096), (2, 144, 272), (16, 2816, 2048), (17, 1040, 1040), (33, 4096, 656),
-          (77, 1424, 4096), (128, 4096, 1024), (129, 272, 384), (200, 2048, 528), (512, 1024, 2064), (1000, 1296, 1152), (3, 512, 14336)]
+SHAPES = FEW + MANY
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -156,8 +156,9 @@ def test_whole_numbers_are_exact(M, N, K):
     assert torch.equal(got.double(), y)
 
 
-def test_strides_of_the_linear_layer():
-    M, N, K = 37, 400, 656
+@pytest.mark.parametrize("M,N", [(37, 400), (300, 400), (2000, 4112)])
+def test_strides_of_the_linear_layer(M, N):
+    K = 656
     g = gen(8)
     x8, s_x = random_rows(g, M, K)
     w8, s_w = random_weights(g, (N, K))
@@ -172,9 +173,9 @@ def test_strides_of_the_linear_layer():
         assert bool((out[:, N:] == 7.0).all())
 
 
-@pytest.mark.parametrize("M", [5, 300])
-def test_what_is_not_finite_stays_in_its_row_or_channel(M):
-    N, K = 272, 528
+@pytest.mark.parametrize("M,N", [(5, 272), (300, 272), (2000, 4112)])
+def test_what_is_not_finite_stays_in_its_row_or_channel(M, N):
+    K = 528
     g = gen(M)
     x8, s_x = random_rows(g, M, K)
     w8, s_w = random_weights(g, (N, K))
@@ -205,12 +206,11 @@ def _offsets(counts, first=0):
     return torch.tensor([first] + counts, device="cuda").cumsum(0).to(torch.int32)
 
 
-COUNTS = [[1], [0, 0, 1], [1, 1, 1, 1, 1, 1, 1, 1], [0, 5, 0, 33, 2, 0, 16, 17], [130, 0, 1, 300, 64], [3] * 40, [129], [0, 257, 0],
-          [700, 500, 3, 0, 250, 128, 127]]
+EXPERTS = [(c, N, K) for c in EXPERTS_FEW for N, K in ((16, 16), (272, 400), (1408, 2048), (128, 4096))] + \
+          [(c, N, K) for c in EXPERTS_MANY for N, K in EXPERTS_MANY_LAYERS]
 
 
-@pytest.mark.parametrize("counts", COUNTS)
-@pytest.mark.parametrize("N,K", [(16, 16), (272, 400), (1408, 2048), (128, 4096)])
+@pytest.mark.parametrize("counts,N,K", EXPERTS)
 def test_experts(counts, N, K):
     rows, E = sum(counts) + 6, len(counts)
     g = gen(sum(counts) + N + K)
