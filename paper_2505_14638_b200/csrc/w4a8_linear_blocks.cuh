@@ -260,12 +260,14 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     } else if (warp == 1) {
         ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), Cfg::kTmemCols);
         ptx::tmem_relinquish();
+        // The next kernel's CTAs may come only once this one's have their tensor memory: they hold theirs until they have run, and
+        // they run only when this kernel is done.
+        ptx::griddep_launch_dependents();
     } else if (warp == 2 && lane == 0) {
         ptx::prefetch_tensormap(&tmap_w);
         ptx::prefetch_tensormap(&tmap_x);
     }
     if (cut > 1) ptx::cluster_arrive_relaxed();   // (behind the barriers' set-up; waited for ahead of the first access to another CTA)
-    ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     ptx::tc_fence_before_sync();
     if (grouped) {
@@ -594,8 +596,8 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
     if (warp == 9) {
         ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), 512);
         ptx::tmem_relinquish_pair();
+        ptx::griddep_launch_dependents();   // (not before: see linear_blocks_kernel)
     }
-    ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     ptx::tc_fence_before_sync();
     if (p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
