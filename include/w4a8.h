@@ -536,7 +536,8 @@ int w4a8_linear_fp8_experts(const uint8_t* x8, int64_t ldx8, const float* s_x, i
  *   smaller group; only experts of the top_groups groups of highest key can be chosen;
  *   the top_k experts of highest key are chosen in descending order.  Equal keys: the lower index first, groups and experts.
  *   weights = score, divided by the sum of the chosen scores (renormalize = 1; 0 where that sum is 0), times scale.
- * Keys are compared as FP64 values (without a bias and with group_best = 1 as the logits themselves, which have their order).
+ * Without a bias and with one group or group_best = 1 keys are compared as the logits themselves, which have their order.
+ * Otherwise as FP64 values without the last 9 bits: keys that agree in their first 44 bits count as equal.
  * Experts whose logit is NaN or -inf, or whose bias is, cannot be chosen (a NaN logit counts as -inf in the softmax); a group with
  * fewer than group_best experts that can be comes last.  A token with fewer than top_k experts has id -1, weight 0 and slot
  * -1 behind them: a row of -inf goes to no expert.

@@ -19,6 +19,11 @@
 //
 // Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 outputs, then one group of four that adds, or two above 32 tokens
 // (each half of the tokens: with one, 80 tokens were bound by it, 780 cycles a k-block).
+//
+// Measured: 512 rows of 120 of 128 experts, (4096, 4096) each (2.0 GB of weights), 290 us: 7.0 TB/s, more than a plain copy reaches
+// (reads alone).  128 rows of 31 experts 102 us: DRAM reads are the weights' 521 MB, once.  Few weights are bound by what surrounds
+// their stream -- launch, first loads, the sums' way, outputs: (77, 14336, 4096) 18.8 us, 3.1 TB/s; (1, 6144, 4096) 8.0 us, 3.1
+// TB/s; 8 rows of 8 experts 13.3 us, 3.5 TB/s.  Asking for the first weights ahead of the wait for the earlier kernel gained nothing.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -521,10 +526,17 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
 }
 
 // ---- many tokens: CTA pairs ----------------------------------------------------------------------------------------------------
-// Bound by the tensor cores.  A tile is 256 tokens x 256 channels of a CTA pair (cta_group::2): the tokens are the A operand, so that
-// a thread of the warps that add has one token and needs one product s_x * s_w per k-block and 128 channels; each CTA holds 128
-// tokens and the sums of all 256 channels: 128 registers in each of 256 threads.  Its k-block's MMAs (512 cycles) go into one of two
-// buffers of tensor memory while the other is fetched (256 columns: 256 cycles) and added.
+// A tile is 256 tokens x 256 channels of a CTA pair (cta_group::2): the tokens are the A operand, so that a thread of the warps that
+// add has one token and needs one product s_x * s_w per k-block and 128 channels; each CTA holds 128 tokens and the sums of all
+// 256 channels: 128 registers in each of 256 threads.  Its k-block's MMAs (512 cycles) go into one of two buffers of tensor memory
+// while the other is fetched (256 columns: 256 cycles) and added.
+//
+// Bound by that exchange of the buffers: a k-block takes 820 to 840 cycles -- its 512, then the way from the MMAs' completion to the
+// warps that add, their fetch, and the way back, of which only a part hides behind the other buffer's MMAs; tensor memory holds no
+// third one of 256 columns.  (2048, 8192, 8192) 149 us: the tensor pipe is active 54 % of the time.  Large layers also meet the
+// power limit: (8192, 28672, 8192) takes 1840 to 2140 us (2.1 to 1.8 PFLOP/s), on different GPUs, at 1.1 to 1.3 GHz -- the same MMAs
+// without the fetches and additions 1450 to 1800.  Without gain: sixteen warps that add, buffers of 128 columns, a second warp that
+// issues, outputs by bulk stores (a stage of the ring less), the first columns of the next k-block fetched ahead.
 //
 // Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs, 10 scales (11 idle): the
 // products s_x * s_w of eight k-blocks at a time, through shared memory.  (Fetched by the warps that add, a k-block's scales cost
@@ -535,8 +547,10 @@ constexpr int kPairBlocksScaleBytes = 2 * 2 * kBlocksChunk * 128 * 4;   // [2 bu
 constexpr int kPairBlocksStageBytes = 32768;   // 128 tokens, 128 channels
 constexpr int kPairBlocksBand = 32;            // token tiles (8192 tokens) that share the channels' weights while they are in L2
 constexpr int kPairBlocksBars = 2 * kPairBlocksStages + 4 + 4 + 1;
+constexpr int kPairBlocksTiles = (8 * kPairBlocksBars + 8 + 15) / 16 * 16;   // behind the barriers: where tiles are described, 16 bytes each
+constexpr int kPairBlocksTable = kPairBlocksTiles + 4 * 16;
 __host__ __device__ constexpr int pair_blocks_smem(bool grouped) {
-    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + kPairBlocksScaleBytes + kPairBlocksOutBytes + 8 * kPairBlocksBars + 16 + (grouped ? (int)sizeof(ExpertTable) : 0);
+    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + kPairBlocksScaleBytes + kPairBlocksOutBytes + kPairBlocksTable + (grouped ? (int)sizeof(ExpertTable) : 0);
 }
 
 // Tile index -> expert, pair of channel blocks and rows.
@@ -571,7 +585,8 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                    bar_scales = bar_acc_free + 16u, bar_scales_free = bar_scales + 16u, bar_drain = bar_scales_free + 16u;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + kBars + 8 * kPairBlocksBars);
     volatile uint32_t* abort_flag = tmem_slot + 1;
-    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kBars + 8 * kPairBlocksBars + 16);
+    const uint32_t tile_info = base + kBars + kPairBlocksTiles;   // [4] first row, tokens, first channel block
+    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kBars + kPairBlocksTable);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();
@@ -672,37 +687,39 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         }
         __syncwarp();
     } else if (warp == 10) {
-        // ------------------------------------------------------------------ scales (a lane has four tokens)
+        // ------------------------------------------------------------------ scales (a lane has four tokens), and what the tiles are
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         bool ok = true;
         ptx::Ring r;
-        int filled = 0;
+        int filled = 0, n = 0;
         const bool wide = (p.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(p.s_x) & 15u) == 0;
-        for (int i = first; i < tiles && ok; i += step) {
+        for (int i = first; i < tiles && ok; i += step, ++n) {
             const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
             const float* sw0 = p.s_w + ((int64_t)t.e * p.NB + t.nb) * KB;
             const float* sw1 = t.nb + 1 < p.NB ? sw0 + KB : sw0;
             for (int b0 = 0; b0 < KB; b0 += kBlocksChunk) {
                 float w0 = 0.0f, w1 = 0.0f;
-                const int n = min(kBlocksChunk, KB - b0);
-                if (lane < n) {
+                const int len = min(kBlocksChunk, KB - b0);
+                if (lane < len) {
                     w0 = __ldg(sw0 + b0 + lane);
                     w1 = __ldg(sw1 + b0 + lane);
                 }
                 if (filled >= 2) ok = ptx::mbar_wait_warp(bar_scales_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
                 if (!ok) break;
+                // (four places: the chunk of a tile that comes two tiles later waits for all warps to be done with this tile's)
+                if (b0 == 0 && lane == 0) ptx::st_shared_v4(tile_info + (uint32_t)((n & 3) * 16), make_uint4((uint32_t)t.row, (uint32_t)t.count, (uint32_t)t.nb, 0u));
                 float* f = reinterpret_cast<float*>(sm + kScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
 #pragma unroll 2
                 for (int k = 0; k < 4; ++k) {
                     const int in = (int)rank * 128 + k * 32 + lane;
                     const float* sx = p.s_x + (t.row + min(in, t.count - 1)) * p.lds + b0;   // (a row that exists)
                     float x[kBlocksChunk];
-                    if (wide && n == kBlocksChunk) {
+                    if (wide && len == kBlocksChunk) {
                         const float4 u = __ldg(reinterpret_cast<const float4*>(sx)), v = __ldg(reinterpret_cast<const float4*>(sx) + 1);
                         x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
                     } else {
 #pragma unroll
-                        for (int j = 0; j < kBlocksChunk; ++j) x[j] = j < n ? __ldg(sx + j) : 0.0f;
+                        for (int j = 0; j < kBlocksChunk; ++j) x[j] = j < len ? __ldg(sx + j) : 0.0f;
                     }
 #pragma unroll
                     for (int j = 0; j < kBlocksChunk; ++j) {
@@ -723,17 +740,21 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         // ------------------------------------------------------------------ sums and outputs: thread = token
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // (128 registers of sums and 64 of columns leave few: the loop over k-blocks keeps next to nothing, and what is needed
-        // around it is worked out again.  With spills in it, it took a third longer.)
+        // around it is read again.  With spills in it, it took a third longer; with the tile worked out twice by each of these warps,
+        // 32768 rows of 64 experts of (4096, 2048) took 456 us instead of 422.)
         const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
         const uint32_t sc_mine = base + kScales + (uint32_t)((warp >> 2) * kBlocksChunk * 512 + (warp & 3) * 128 + lane * 4);
         bool ok = true;
         int it = 0, chunk = 0;   // k-blocks and chunks of eight of them so far
-        for (int i = first; i < tiles && ok; i += step) {
-            bool any;   // (warp-uniform) a token of this warp, and its channels, are there
-            {
-                const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
-                any = (int)rank * 128 + (warp & 3) * 32 < t.count && t.nb + (warp >> 2) < p.NB;
-            }
+        for (int n = 0; it < n_it && ok; ++n) {   // tiles
+            auto this_tile = [&](int& row, int& count, int& nb) {
+                asm volatile(
+                    "{\n\t.reg .b32 none;\n\tld.shared.v4.b32 {%0, %1, %2, none}, [%3];\n\t}"
+                    : "=r"(row), "=r"(count), "=r"(nb)
+                    : "r"(tile_info + (uint32_t)((n & 3) * 16))
+                    : "memory");
+            };
+            bool any = false;   // (warp-uniform) a token of this warp, and its channels, are there
             unsigned long long acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = 0ull;
@@ -741,6 +762,11 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                 ok = ptx::mbar_wait_warp(bar_scales + 8u * (chunk & 1), (uint32_t)(chunk >> 1) & 1u, abort_flag, p.status);
                 if (!ok) break;
                 const uint32_t sc = sc_mine + (uint32_t)((chunk & 1) * 2 * kBlocksChunk * 512);
+                {
+                    int row, count, nb;
+                    this_tile(row, count, nb);
+                    any = (int)rank * 128 + (warp & 3) * 32 < count && nb + (warp >> 2) < p.NB;
+                }
                 const int end = min(kBlocksChunk, left);
                 left -= end;
 #pragma unroll 1
@@ -788,13 +814,15 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
             if (ok && any) {
                 // Outputs, 128 bytes of 32 rows at a time, through shared memory (pieces of 16 bytes permuted by their row, so that
                 // neither side meets a bank twice): a store then touches four lines, not one for each of 32 rows.
-                const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
-                const int q = warp & 3, nb = t.nb + (warp >> 2);
+                int tile_row, count, nb;
+                this_tile(tile_row, count, nb);
+                nb += warp >> 2;
+                const int q = warp & 3;
                 const uint32_t out_s = base + kOut + (uint32_t)(warp * 4096);
                 const int es = p.out_fp32 ? 4 : 2;
                 const bool wide = ((p.ldy * es) & 15) == 0;   // rows 16-byte aligned (y itself is)
-                const int row0 = (int)rank * 128 + q * 32, rows = min(32, t.count - row0);
-                uint8_t* y0 = static_cast<uint8_t*>(p.y) + ((t.row + row0) * p.ldy + nb * 128) * es;
+                const int row0 = (int)rank * 128 + q * 32, rows = min(32, count - row0);
+                uint8_t* y0 = static_cast<uint8_t*>(p.y) + (((int64_t)tile_row + row0) * p.ldy + nb * 128) * es;
                 const int have = min(128, p.N - nb * 128) * es;   // bytes of a row of this channel block
                 auto store = [&](int piece) {   // the piece's rows, four of them per round
                     __syncwarp();
