@@ -86,10 +86,11 @@ static int quantize_blocks_impl(const void* x, int64_t M, int64_t K, int64_t ldx
 }
 
 // ------------------------------------------------------------------------------ linear layers
-static bool make_map(CUtensorMap* m, const void* ptr, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+static bool make_map(CUtensorMap* m, const void* ptr, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                     CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_UINT8) {
     EncodeTiledFn fn = encode_tiled_fn();
     const cuuint32_t step[3] = {1, 1, 1};
-    return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<void*>(ptr), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn && fn(m, type, rank, const_cast<void*>(ptr), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -157,7 +158,14 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
         static std::atomic<uint64_t> allowed{0};
         if (!allow_smem(linear_blocks_pair_kernel, allowed)) return W4A8_ERR_CUDA;
         const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
-        return launch(linear_blocks_pair_kernel, (unsigned)(2 * pairs), kPairBlocksThreads, (size_t)pair_blocks_smem(offsets != nullptr), 2, st, tw, tx, p);
+        CUtensorMap ty = tx;   // (not used where rows of y are not 16-byte aligned)
+        const int es = p.out_fp32 ? 4 : 2;
+        if (ldy * es % 16 == 0) {
+            const cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(ldy * es)};
+            const cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32};
+            if (!make_map(&ty, y, 2, dims, strides, box, p.out_fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16)) return W4A8_ERR_CUDA;
+        }
+        return launch(linear_blocks_pair_kernel, (unsigned)(2 * pairs), kPairBlocksThreads, (size_t)pair_blocks_smem(offsets != nullptr), 2, st, tw, tx, ty, p);
     }
     p.channels = pl.channels;
     p.row_tiles = (int)ceil_div(N, pl.channels);

@@ -536,7 +536,7 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
 // third one of 256 columns.  (2048, 8192, 8192) 149 us: the tensor pipe is active 54 % of the time.  Large layers also meet the
 // power limit: (8192, 28672, 8192) takes 1840 to 2140 us (2.1 to 1.8 PFLOP/s), on different GPUs, at 1.1 to 1.3 GHz -- the same MMAs
 // without the fetches and additions 1450 to 1800.  Without gain: sixteen warps that add, buffers of 128 columns, a second warp that
-// issues, outputs by bulk stores (a stage of the ring less), the first columns of the next k-block fetched ahead.
+// issues, the first columns of the next k-block fetched ahead.
 //
 // Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs, 10 scales (11 idle): the
 // products s_x * s_w of eight k-blocks at a time, through shared memory.  (Fetched by the warps that add, a k-block's scales cost
@@ -573,6 +573,7 @@ __device__ __forceinline__ BlocksTile pair_blocks_tile(const BlocksParams& p, co
 __global__ void __launch_bounds__(kPairBlocksThreads, 1)
 linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
                           const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 128, 128B swizzle
+                          const __grid_constant__ CUtensorMap tmap_y,   // y [rows][N] where its rows are 16-byte aligned, box 128 bytes x 32, 128B swizzle
                           const BlocksParams p) {
     constexpr int S = kPairBlocksStages;
     extern __shared__ uint8_t smem_raw[];
@@ -812,8 +813,10 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                 if (lane == 0) ptx::mbar_arrive(bar_scales_free + 8u * (chunk & 1));
             }
             if (ok && any) {
-                // Outputs, 128 bytes of 32 rows at a time, through shared memory (pieces of 16 bytes permuted by their row, so that
-                // neither side meets a bank twice): a store then touches four lines, not one for each of 32 rows.
+                // Outputs, 128 bytes of 32 rows at a time, through shared memory (pieces of 16 bytes permuted by their row as in the 128-byte
+                // swizzle, so that neither side meets a bank twice) and from there by bulk stores: read back and stored by the warps,
+                // 32768 rows of 64 experts of (4096, 2048) took 420 us instead of 406.  Where a bulk store would write rows behind an
+                // expert's last, or y's rows are not 16-byte aligned, the warps store; an instruction then touches four lines.
                 int tile_row, count, nb;
                 this_tile(tile_row, count, nb);
                 nb += warp >> 2;
@@ -824,7 +827,17 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                 const int row0 = (int)rank * 128 + q * 32, rows = min(32, count - row0);
                 uint8_t* y0 = static_cast<uint8_t*>(p.y) + (((int64_t)tile_row + row0) * p.ldy + nb * 128) * es;
                 const int have = min(128, p.N - nb * 128) * es;   // bytes of a row of this channel block
+                const bool bulk = wide && (rows == 32 || p.offsets == nullptr);
                 auto store = [&](int piece) {   // the piece's rows, four of them per round
+                    if (bulk) {
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && piece * 128 < have) {
+                            ptx::tma_store_2d(&tmap_y, nb * 128 + piece * (128 / es), tile_row + row0, out_s);
+                            ptx::bulk_commit();
+                        }
+                        return;
+                    }
                     __syncwarp();
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -851,9 +864,14 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                     __syncwarp();
                 };
                 const uint32_t mine = out_s + (uint32_t)(lane * 128);
+                auto room = [&]() {   // bulk stores have read what is written over next
+                    if (lane == 0) ptx::bulk_wait_read();
+                    __syncwarp();
+                };
                 if (p.out_fp32) {
 #pragma unroll
                     for (int piece = 0; piece < 4; ++piece) {
+                        room();
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             float f[4];
@@ -877,6 +895,7 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                                 const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
                                 o[k] = *reinterpret_cast<const uint32_t*>(&h);
                             }
+                            if (c == 0) room();
                             ptx::st_shared_v4(mine + (uint32_t)(((c ^ lane) & 7) << 4), make_uint4(o[0], o[1], o[2], o[3]));
                         }
                         store(piece);
@@ -886,6 +905,8 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         }
     }
 
+    if (lane == 0) ptx::bulk_wait();   // (outputs)
+    __syncwarp();
     ptx::tc_fence_before_sync();
     __syncthreads();
     // Closing barrier: neither CTA leaves while the other may still reach into its shared memory or barriers.  What is sent to
