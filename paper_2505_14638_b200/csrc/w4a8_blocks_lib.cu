@@ -125,18 +125,18 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     if (sms <= 0 || !status) return W4A8_ERR_CUDA;
     const BlocksPlan pl = blocks_plan(rows, experts, N, K, sms, offsets != nullptr);
     // (with experts: at most)
-    const int64_t tiles = ceil_div(N, pl.pair ? 256 : pl.channels) * (ceil_div(rows, pl.tokens) + (offsets ? experts : 0));
+    const int64_t tiles = ceil_div(N, pl.wide ? 256 : pl.channels) * (ceil_div(rows, pl.tokens) + (offsets ? experts : 0));
     if (tiles > INT32_MAX / 2) return W4A8_ERR_BAD_SHAPE;
     CUtensorMap tw, tx;
     {
         const cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)experts};
         const cuuint64_t strides[2] = {(cuuint64_t)ldw, (cuuint64_t)(experts > 1 ? w_stride : N * ldw)};
-        const cuuint32_t box[3] = {128, pl.pair ? 128u : (cuuint32_t)pl.channels, 1};
+        const cuuint32_t box[3] = {128, pl.wide ? 128u : (cuuint32_t)pl.channels, 1};
         if (!make_map(&tw, w8, 3, dims, strides, box)) return W4A8_ERR_CUDA;
     }
     {
         const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ldx8};
-        const cuuint32_t box[2] = {128, pl.pair ? 128u : 32u};
+        const cuuint32_t box[2] = {128, pl.wide ? 128u : 32u};
         if (!make_map(&tx, x8, 2, dims, strides, box)) return W4A8_ERR_CUDA;
     }
     BlocksParams p = {};
@@ -154,10 +154,7 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
     p.tokens = pl.tokens;
     p.out_fp32 = out_dtype == W4A8_OUT_FP32 ? 1 : 0;
     p.status = status;
-    if (pl.pair) {
-        static std::atomic<uint64_t> allowed{0};
-        if (!allow_smem(linear_blocks_pair_kernel, allowed)) return W4A8_ERR_CUDA;
-        const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
+    if (pl.wide) {
         CUtensorMap ty = tx;   // (not used where rows of y are not 16-byte aligned)
         const int es = p.out_fp32 ? 4 : 2;
         if (ldy * es % 16 == 0) {
@@ -165,7 +162,9 @@ static int linear_blocks_impl(const uint8_t* x8, int64_t ldx8, const float* s_x,
             const cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32};
             if (!make_map(&ty, y, 2, dims, strides, box, p.out_fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16)) return W4A8_ERR_CUDA;
         }
-        return launch(linear_blocks_pair_kernel, (unsigned)(2 * pairs), kPairBlocksThreads, (size_t)pair_blocks_smem(offsets != nullptr), 2, st, tw, tx, ty, p);
+        static std::atomic<uint64_t> allowed{0};
+        if (!allow_smem(linear_blocks_wide_kernel, allowed)) return W4A8_ERR_CUDA;
+        return launch(linear_blocks_wide_kernel, (unsigned)(tiles < sms ? tiles : sms), kWideThreads, (size_t)wide_smem(offsets != nullptr), 1, st, tw, tx, ty, p);
     }
     p.channels = pl.channels;
     p.row_tiles = (int)ceil_div(N, pl.channels);

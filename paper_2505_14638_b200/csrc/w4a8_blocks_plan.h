@@ -41,7 +41,7 @@ W4A8_BOTH inline BlocksSmem blocks_smem(int tmax, int channels, int tokens, int 
 }
 
 struct BlocksPlan {
-    bool pair;         // CTA pairs: tiles of 256 tokens x 256 channels
+    bool wide;         // tiles of 128 tokens x 256 channels
     int tmax;          // tokens that the kernel's registers are laid out for: 16, 32, 64, 128
     int tokens;        // tokens of a tile at most
     int channels;      // channels of a tile
@@ -75,8 +75,10 @@ inline bool blocks_fit(BlocksPlan* pl, int64_t rounds, bool grouped) {
 // takes each row to go to any of them, and an expert to have up to four times the average.
 //
 // Costs are in units of an SM's share of HBM for a k-block of 128 channels (16 KB, 0.37 us), without what every launch takes.
-// Measured, us, tiles of up to 128 tokens / pairs: (256, 4096, 4096) 15.4 / 22.4, (512, 1024, 4096) 11.3 / 21.6, (256, 14336, 4096)
-// 37.5 / 24.8, (1024, 4096, 4096) 37.3 / 24.0; 64 experts of (4096, 2048) with 64, 128, 256 rows each 128 / 148, 195 / 163, 355 / 221.
+// Measured, us, tiles of up to 128 channels / of 256: (128, 4096, 4096) 11.6 / 21.6, (77, 14336, 4096) 19.7 / 22.5, (128, 28672, 8192)
+// 78.0 / 50.6, (256, 14336, 4096) 38.1 / 24.0, (512, 4096, 4096) 20.8 / 21.2, (1024, 4096, 4096) 37.5 / 22.0; 64 experts of (4096,
+// 2048) with 32, 64, 128 rows each 133 / 98, 166 / 108, 256 / 134; 128 of (6928, 896) with 6 rows each 194 / 143, of (4096, 4096) with 4
+// rows each 291 / 309.
 inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t K, int sms, bool grouped) {
     const int64_t KB = ceil_div(K, 128);
     int64_t with_rows = 1, load = rows;
@@ -135,12 +137,15 @@ inline BlocksPlan blocks_plan(int64_t rows, int64_t experts, int64_t N, int64_t 
     if (cut > 8) cut = 8;
     if (cut > KB / 2) cut = KB / 2;
     while (cut >= 2 && !consider(128, (int)cut)) --cut;
-    if (tmax == 128 && rows > 128) {
-        const int64_t tiles = ceil_div(N, 256) * token_tiles(256);
-        if (rounds_of(tiles, sms / 2) * ((double)KB * 1.23 + 4.0) < least) {
+    if (tmax >= 64 && rows > 64 && N > 128) {
+        const int64_t of_tokens = token_tiles(128), tiles = ceil_div(N, 256) * of_tokens;
+        // weights of a k-block: from HBM for one of an expert's (or the layer's) token tiles, from L2 for the others
+        const double stream = 2.0 * (double)with_rows / (double)of_tokens * (tiles < sms ? (double)tiles / sms : 1.0);
+        const double work = (double)KB * 1.25 + 4.3, wait = (double)KB * stream + 0.8;
+        if (rounds_of(tiles, sms) * (work > wait ? work : wait) < least) {
             best = {};
-            best.pair = true;
-            best.tokens = 256;
+            best.wide = true;
+            best.tokens = 128;
             best.tiles = tiles;
         }
     }

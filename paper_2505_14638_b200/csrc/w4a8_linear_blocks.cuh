@@ -121,7 +121,7 @@ __device__ __forceinline__ void fill_expert_table(ExpertTable* t, const int32_t*
 
 // A tile: expert, rows, and where its channels begin.
 struct BlocksTile {
-    int e, nb, count;   // expert; first channel block (pairs) or first channel; tokens
+    int e, nb, count;   // expert; first channel block (many tokens) or first channel; tokens
     int64_t row;        // first row
 };
 // The rows of token tile j.
@@ -525,36 +525,36 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
     }
 }
 
-// ---- many tokens: CTA pairs ----------------------------------------------------------------------------------------------------
-// A tile is 256 tokens x 256 channels of a CTA pair (cta_group::2): the tokens are the A operand, so that a thread of the warps that
-// add has one token and needs one product s_x * s_w per k-block and 128 channels; each CTA holds 128 tokens and the sums of all
-// 256 channels: 128 registers in each of 256 threads.  Its k-block's MMAs (512 cycles) go into one of two buffers of tensor memory
-// while the other is fetched (256 columns: 256 cycles) and added.
+// ---- many tokens ---------------------------------------------------------------------------------------------------------------
+// A tile is 128 tokens x 256 channels: the tokens are the A operand, so that a thread of the warps that add has one token and needs
+// one product s_x * s_w per k-block and 128 channels.  The sums of a tile are 128 registers in each of 256 threads; a k-block's MMAs
+// (512 cycles) go into one of two buffers of tensor memory while the other is fetched (256 columns: 256 cycles) and added.
 //
-// Bound by that exchange of the buffers: a k-block takes 820 to 840 cycles -- its 512, then the way from the MMAs' completion to the
-// warps that add, their fetch, and the way back, of which only a part hides behind the other buffer's MMAs; tensor memory holds no
-// third one of 256 columns.  (2048, 8192, 8192) 149 us: the tensor pipe is active 54 % of the time.  Large layers also meet the
-// power limit: (8192, 28672, 8192) takes 1840 to 2140 us (2.1 to 1.8 PFLOP/s), on different GPUs, at 1.1 to 1.3 GHz -- the same MMAs
-// without the fetches and additions 1450 to 1800.  Without gain: sixteen warps that add, buffers of 128 columns, a second warp that
-// issues, the first columns of the next k-block fetched ahead.
+// Bound by that exchange of the buffers -- a k-block's 512 cycles, then the way from the MMAs' completion to the warps that add, their
+// fetch and the way back, of which only a part hides behind the other buffer's MMAs; tensor memory holds no third one of 256 columns --
+// and, where a launch lasts, by the power limit.  (2048, 8192, 8192) 146 us, 1.9 PFLOP/s; (8192, 8192, 4096) 264 us, 2.1 PFLOP/s;
+// (8192, 28672, 8192) 1970 us, 1.95 PFLOP/s, at 1.1 to 1.3 GHz.  Tiles of 256 x 256 on pairs of CTAs, each with half of the channels'
+// weights, load two thirds of this, but their buffers' way back leads through the other CTA, and experts fill them worse: 158, 282 and
+// 2190 us; 64 experts of (4096, 2048) with 512 rows each 379 us instead of 334, with 128 rows 186 instead of 134.  Without gain on
+// pairs: sixteen warps that add, buffers of 128 columns, a second warp that issues, the first columns of the next k-block fetched ahead.
 //
 // Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs, 10 scales (11 idle): the
 // products s_x * s_w of eight k-blocks at a time, through shared memory.  (Fetched by the warps that add, a k-block's scales cost
 // each of them a load of 32 lines, and its latency.)
-constexpr int kPairBlocksThreads = 384, kPairBlocksStages = 5;
-constexpr int kPairBlocksOutBytes = 8 * 4096;  // outputs on their way, 32 rows of 128 bytes per warp
-constexpr int kPairBlocksScaleBytes = 2 * 2 * kBlocksChunk * 128 * 4;   // [2 buffers][2 channel blocks][k-block][token]
-constexpr int kPairBlocksStageBytes = 32768;   // 128 tokens, 128 channels
-constexpr int kPairBlocksBand = 32;            // token tiles (8192 tokens) that share the channels' weights while they are in L2
-constexpr int kPairBlocksBars = 2 * kPairBlocksStages + 4 + 4 + 1;
-constexpr int kPairBlocksTiles = (8 * kPairBlocksBars + 8 + 15) / 16 * 16;   // behind the barriers: where tiles are described, 16 bytes each
-constexpr int kPairBlocksTable = kPairBlocksTiles + 4 * 16;
-__host__ __device__ constexpr int pair_blocks_smem(bool grouped) {
-    return 1024 + kPairBlocksStages * kPairBlocksStageBytes + kPairBlocksScaleBytes + kPairBlocksOutBytes + kPairBlocksTable + (grouped ? (int)sizeof(ExpertTable) : 0);
-}
+constexpr int kWideThreads = 384, kWideTokens = 128, kWideStages = 3;
+constexpr int kWideStageBytes = 16384 + 32768;                          // 128 tokens, 256 channels
+constexpr int kWideScaleBytes = 2 * 2 * kBlocksChunk * 128 * 4;         // [2 buffers][2 channel blocks][k-block][token]
+constexpr int kWideOutBytes = 8 * 4096;                                 // outputs on their way, 32 rows of 128 bytes per warp
+constexpr int kWideScales = kWideStages * kWideStageBytes, kWideOut = kWideScales + kWideScaleBytes, kWideBars = kWideOut + kWideOutBytes;
+constexpr int kWideNumBars = 2 * kWideStages + 4 + 4 + 1;
+constexpr int kWideTiles = kWideBars + (8 * kWideNumBars + 8 + 15) / 16 * 16;   // where tiles are described, 16 bytes each
+constexpr int kWideTable = kWideTiles + 4 * 16;
+constexpr int kWideBand = 64;                                           // token tiles (8192 tokens) that share the channels' weights while they are in L2
+constexpr int wide_smem(bool grouped) { return 1024 + kWideTable + (grouped ? (int)sizeof(ExpertTable) : 0); }
+static_assert(wide_smem(true) <= kBlocksSmemMax, "shared memory");
 
-// Tile index -> expert, pair of channel blocks and rows.
-__device__ __forceinline__ BlocksTile pair_blocks_tile(const BlocksParams& p, const ExpertTable* t, int i, int token_tiles) {
+// Tile index -> expert, first of two channel blocks and rows.
+__device__ __forceinline__ BlocksTile wide_blocks_tile(const BlocksParams& p, const ExpertTable* t, int i, int token_tiles) {
     const int NT = (p.NB + 1) >> 1;
     BlocksTile b;
     if (p.offsets != nullptr) {
@@ -563,35 +563,32 @@ __device__ __forceinline__ BlocksTile pair_blocks_tile(const BlocksParams& p, co
         b.nb = 2 * (i - j * NT);
         return b;
     }
-    const int per = kPairBlocksBand * NT, band = i / per, in = i - band * per;
-    const int high = min(kPairBlocksBand, token_tiles - band * kPairBlocksBand), n = in / high;
-    b = blocks_rows(p, t, band * kPairBlocksBand + in - n * high);
+    const int per = kWideBand * NT, band = i / per, in = i - band * per;
+    const int high = min(kWideBand, token_tiles - band * kWideBand), n = in / high;
+    b = blocks_rows(p, t, band * kWideBand + in - n * high);
     b.nb = 2 * n;
     return b;
 }
 
-__global__ void __launch_bounds__(kPairBlocksThreads, 1)
-linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
+__global__ void __launch_bounds__(kWideThreads, 1)
+linear_blocks_wide_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][K], box 128 x 128 x 1, 128B swizzle
                           const __grid_constant__ CUtensorMap tmap_x,   // x8 [rows][K], box 128 x 128, 128B swizzle
                           const __grid_constant__ CUtensorMap tmap_y,   // y [rows][N] where its rows are 16-byte aligned, box 128 bytes x 32, 128B swizzle
                           const BlocksParams p) {
-    constexpr int S = kPairBlocksStages;
+    constexpr int S = kWideStages;
+    constexpr uint32_t kStageBytes = (uint32_t)kWideStageBytes;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     const uint32_t base = (raw_addr + 1023u) & ~1023u;
     uint8_t* sm = smem_raw + (base - raw_addr);
-    constexpr uint32_t kScales = (uint32_t)(S * kPairBlocksStageBytes), kOut = kScales + (uint32_t)kPairBlocksScaleBytes,
-                       kBars = kOut + (uint32_t)kPairBlocksOutBytes;
-    const uint32_t bar_full = base + kBars, bar_free = bar_full + 8u * S, bar_acc = bar_free + 8u * S, bar_acc_free = bar_acc + 16u,
+    const uint32_t bar_full = base + (uint32_t)kWideBars, bar_free = bar_full + 8u * S, bar_acc = bar_free + 8u * S, bar_acc_free = bar_acc + 16u,
                    bar_scales = bar_acc_free + 16u, bar_scales_free = bar_scales + 16u, bar_drain = bar_scales_free + 16u;
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + kBars + 8 * kPairBlocksBars);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + kWideBars + 8 * kWideNumBars);
     volatile uint32_t* abort_flag = tmem_slot + 1;
-    const uint32_t tile_info = base + kBars + kPairBlocksTiles;   // [4] first row, tokens, first channel block
-    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kBars + kPairBlocksTable);
+    const uint32_t tile_info = base + (uint32_t)kWideTiles;   // [4] first row, tokens, first channel block
+    ExpertTable* table = reinterpret_cast<ExpertTable*>(sm + kWideTable);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = ptx::cluster_ctarank();
-    const bool leader = rank == 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) {
             ptx::mbar_init(bar_full + 8u * i, 1);
@@ -599,7 +596,7 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         }
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(bar_acc + 8u * i, 1);
-            ptx::mbar_init(bar_acc_free + 8u * i, 16);   // eight warps of each CTA
+            ptx::mbar_init(bar_acc_free + 8u * i, 8);
             ptx::mbar_init(bar_scales + 8u * i, 1);
             ptx::mbar_init(bar_scales_free + 8u * i, 8);
         }
@@ -610,21 +607,20 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         ptx::prefetch_tensormap(&tmap_x);
     }
     if (warp == 9) {
-        ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), 512);
-        ptx::tmem_relinquish_pair();
+        ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), 512);
+        ptx::tmem_relinquish();
         ptx::griddep_launch_dependents();   // (not before: see linear_blocks_kernel)
     }
     ptx::griddep_wait();
     ptx::tc_fence_before_sync();
     if (p.offsets != nullptr) fill_expert_table(table, p.offsets, p.E, p.rows, p.tokens);
     else __syncthreads();
-    ptx::cluster_sync_all();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     const int token_tiles = p.offsets != nullptr ? table->tile[p.E] : (int)((p.rows + p.tokens - 1) / p.tokens);
     const int tiles = token_tiles * ((p.NB + 1) >> 1);
-    const int first = (int)blockIdx.x >> 1, step = (int)gridDim.x >> 1, KB = p.KB;
-    const int n_it = first < tiles ? ((tiles - first + step - 1) / step) * KB : 0;   // k-blocks of all tiles of this pair
+    const int first = (int)blockIdx.x, step = (int)gridDim.x, KB = p.KB;
+    const int n_it = first < tiles ? ((tiles - first + step - 1) / step) * KB : 0;   // k-blocks of all tiles of this CTA
 
     if (warp == 8) {
         // ------------------------------------------------------------------ loads (whole warp, one lane issues)
@@ -634,22 +630,22 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         ptx::Ring r;
         int issued = 0;
         for (int i = first; i < tiles && ok; i += step) {
-            const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
-            const int y = (int)t.row + (int)rank * 128, n = t.nb * 128 + (int)rank * 128;
+            const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
             for (int b = 0; b < KB; ++b) {
                 if (issued >= S) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
                 if (!ok) break;
-                const uint32_t full = bar_full + 8u * r.idx, to = ptx::map_to_cta(full, 0u), dst = base + (uint32_t)(r.idx * kPairBlocksStageBytes);
-                if (ptx::elect_one()) {
-                    if (leader) ptx::mbar_arrive_expect_tx(full, 2u * kPairBlocksStageBytes);
-                    ptx::tma_load_2d_pair(dst, &tmap_x, b * 128, y, to);
-                    ptx::tma_load_3d_pair(dst + 16384u, &tmap_w, b * 128, n, t.e, to);
+                const uint32_t full = bar_full + 8u * r.idx, dst = base + (uint32_t)r.idx * kStageBytes;
+                if (ptx::elect_one()) {   // (channels and rows that are not there come as zeros)
+                    ptx::mbar_arrive_expect_tx(full, kStageBytes);
+                    ptx::tma_load_2d(dst, &tmap_x, b * 128, (int)t.row, full);
+                    ptx::tma_load_3d(dst + 16384u, &tmap_w, b * 128, t.nb * 128, t.e, full);
+                    ptx::tma_load_3d(dst + 32768u, &tmap_w, b * 128, t.nb * 128 + 128, t.e, full);
                 }
                 r.advance(S);
                 ++issued;
             }
         }
-        if (!ok && leader && lane == 0) {   // gave up: let both CTAs' copies in flight land before either goes away
+        if (!ok && lane == 0) {   // gave up: let the copies in flight land before the CTA goes away
             const uint64_t t0 = ptx::globaltimer_ns();
             for (int i = issued > S ? issued - S : 0; i < issued; ++i)
                 while (!ptx::mbar_try_wait(bar_full + 8u * (i % S), (uint32_t)((i / S) & 1)) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 20) {
@@ -657,33 +653,31 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         }
         __syncwarp();
     } else if (warp == 9) {
-        // ------------------------------------------------------------------ MMAs (one lane of the leader issues)
+        // ------------------------------------------------------------------ MMAs (whole warp, one lane issues)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (leader) {
-            constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(256, 256);
-            bool ok = true;
-            ptx::Ring r, a;
-            for (int it = 0; it < n_it; ++it) {
-                // (the buffer is waited for last: it is what comes last)
-                ok = ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
-                if (it >= 2) ok = ok && ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
-                if (!ok) break;
-                ptx::tc_fence_after_sync();
-                const uint32_t s = base + (uint32_t)(r.idx * kPairBlocksStageBytes);
-                const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
-                if (ptx::elect_one()) {
-                    ptx::umma_f8_kblock_pair(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
-                    ptx::umma_commit_pair(bar_acc + 8u * a.idx, 3);
-                    if (it + S < n_it) ptx::umma_commit_pair(bar_free + 8u * r.idx, 3);   // (the slot is used again: see the closing barrier)
-                }
-                r.advance(S);
-                a.advance(2);
+        constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(kWideTokens, 256);
+        bool ok = true;
+        ptx::Ring r, a;
+        for (int it = 0; it < n_it; ++it) {
+            // (the buffer is waited for last: it is what comes last)
+            ok = ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+            if (it >= 2) ok = ok && ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            const uint32_t s = base + (uint32_t)r.idx * kStageBytes;
+            const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
+            if (ptx::elect_one()) {
+                ptx::umma_f8_kblock(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
+                ptx::umma_commit(bar_acc + 8u * a.idx);
+                ptx::umma_commit(bar_free + 8u * r.idx);
             }
-            if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
-                ptx::umma_commit_pair(bar_drain, 1);
-                const uint64_t t0 = ptx::globaltimer_ns();
-                while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
-                }
+            r.advance(S);
+            a.advance(2);
+        }
+        if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
+            ptx::umma_commit(bar_drain);
+            const uint64_t t0 = ptx::globaltimer_ns();
+            while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
             }
         }
         __syncwarp();
@@ -695,7 +689,7 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         int filled = 0, n = 0;
         const bool wide = (p.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(p.s_x) & 15u) == 0;
         for (int i = first; i < tiles && ok; i += step, ++n) {
-            const BlocksTile t = pair_blocks_tile(p, table, i, token_tiles);
+            const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
             const float* sw0 = p.s_w + ((int64_t)t.e * p.NB + t.nb) * KB;
             const float* sw1 = t.nb + 1 < p.NB ? sw0 + KB : sw0;
             for (int b0 = 0; b0 < KB; b0 += kBlocksChunk) {
@@ -709,10 +703,10 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                 if (!ok) break;
                 // (four places: the chunk of a tile that comes two tiles later waits for all warps to be done with this tile's)
                 if (b0 == 0 && lane == 0) ptx::st_shared_v4(tile_info + (uint32_t)((n & 3) * 16), make_uint4((uint32_t)t.row, (uint32_t)t.count, (uint32_t)t.nb, 0u));
-                float* f = reinterpret_cast<float*>(sm + kScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
+                float* f = reinterpret_cast<float*>(sm + kWideScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
 #pragma unroll 2
                 for (int k = 0; k < 4; ++k) {
-                    const int in = (int)rank * 128 + k * 32 + lane;
+                    const int in = k * 32 + lane;
                     const float* sx = p.s_x + (t.row + min(in, t.count - 1)) * p.lds + b0;   // (a row that exists)
                     float x[kBlocksChunk];
                     if (wide && len == kBlocksChunk) {
@@ -742,9 +736,9 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // (128 registers of sums and 64 of columns leave few: the loop over k-blocks keeps next to nothing, and what is needed
         // around it is read again.  With spills in it, it took a third longer; with the tile worked out twice by each of these warps,
-        // 32768 rows of 64 experts of (4096, 2048) took 456 us instead of 422.)
+        // it took 8 % longer for 32768 rows of 64 experts of (4096, 2048).)
         const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
-        const uint32_t sc_mine = base + kScales + (uint32_t)((warp >> 2) * kBlocksChunk * 512 + (warp & 3) * 128 + lane * 4);
+        const uint32_t sc_mine = base + (uint32_t)kWideScales + (uint32_t)((warp >> 2) * kBlocksChunk * 512 + (warp & 3) * 128 + lane * 4);
         bool ok = true;
         int it = 0, chunk = 0;   // k-blocks and chunks of eight of them so far
         for (int n = 0; it < n_it && ok; ++n) {   // tiles
@@ -766,7 +760,7 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                 {
                     int row, count, nb;
                     this_tile(row, count, nb);
-                    any = (int)rank * 128 + (warp & 3) * 32 < count && nb + (warp >> 2) < p.NB;
+                    any = (warp & 3) * 32 < count && nb + (warp >> 2) < p.NB;
                 }
                 const int end = min(kBlocksChunk, left);
                 left -= end;
@@ -781,7 +775,7 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
                     auto release = [&]() {   // the buffer has been read
                         ptx::tc_fence_before_sync();
                         __syncwarp();
-                        if (lane == 0 && it + 2 < n_it) ptx::mbar_arrive_cluster(ptx::map_to_cta(bar_acc_free + 8u * (it & 1), 0u));
+                        if (lane == 0 && it + 2 < n_it) ptx::mbar_arrive(bar_acc_free + 8u * (it & 1));
                     };
                     if (any) {
                         // 32 columns are on their way while those before are added
@@ -815,16 +809,16 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
             if (ok && any) {
                 // Outputs, 128 bytes of 32 rows at a time, through shared memory (pieces of 16 bytes permuted by their row as in the 128-byte
                 // swizzle, so that neither side meets a bank twice) and from there by bulk stores: read back and stored by the warps,
-                // 32768 rows of 64 experts of (4096, 2048) took 420 us instead of 406.  Where a bulk store would write rows behind an
+                // that took 3 % longer for 32768 rows of 64 experts of (4096, 2048).  Where a bulk store would write rows behind an
                 // expert's last, or y's rows are not 16-byte aligned, the warps store; an instruction then touches four lines.
                 int tile_row, count, nb;
                 this_tile(tile_row, count, nb);
                 nb += warp >> 2;
                 const int q = warp & 3;
-                const uint32_t out_s = base + kOut + (uint32_t)(warp * 4096);
+                const uint32_t out_s = base + (uint32_t)(kWideOut + warp * 4096);
                 const int es = p.out_fp32 ? 4 : 2;
                 const bool wide = ((p.ldy * es) & 15) == 0;   // rows 16-byte aligned (y itself is)
-                const int row0 = (int)rank * 128 + q * 32, rows = min(32, count - row0);
+                const int row0 = q * 32, rows = min(32, count - row0);
                 uint8_t* y0 = static_cast<uint8_t*>(p.y) + (((int64_t)tile_row + row0) * p.ldy + nb * 128) * es;
                 const int have = min(128, p.N - nb * 128) * es;   // bytes of a row of this channel block
                 const bool bulk = wide && (rows == 32 || p.offsets == nullptr);
@@ -909,19 +903,9 @@ linear_blocks_pair_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
     __syncwarp();
     ptx::tc_fence_before_sync();
     __syncthreads();
-    // Closing barrier: neither CTA leaves while the other may still reach into its shared memory or barriers.  What is sent to
-    // the other CTA has been waited for there: stages and freed buffers by the MMA warp (freed buffers are not announced after
-    // the last use), freed stages by the load warps (the same), complete buffers by the warps that add.
-    ptx::cluster_sync_all();
-    if (*abort_flag != 0u) {   // (not all of it, after a wait that gave up: late arrivals have 2 ms)
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 1000) {
-        }
-    }
-    __syncwarp();
     if (warp == 9) {
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc_pair(tmem, 512);
+        ptx::tmem_dealloc(tmem, 512);
     }
 }
 

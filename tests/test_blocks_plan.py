@@ -18,12 +18,12 @@ int main() {
     while (std::scanf("%lld %lld %lld %lld %lld %lld", &rows, &experts, &N, &K, &sms, &grouped) == 6) {
         const BlocksPlan p = blocks_plan(rows, experts, N, K, (int)sms, grouped != 0);
         const BlocksSmem s = blocks_smem(p.tmax, p.channels, p.tokens, p.stages, p.cut, p.share, p.part_buffers, grouped != 0);
-        std::printf("%d %d %d %d %d %d %d %d %d %d %lld %d %d %d %d %d\n", p.pair, p.tmax, p.tokens, p.channels, p.cut, p.share, p.part_buffers,
+        std::printf("%d %d %d %d %d %d %d %d %d %d %lld %d %d %d %d %d\n", p.wide, p.tmax, p.tokens, p.channels, p.cut, p.share, p.part_buffers,
                     p.stages, p.smem, p.ctas, (long long)p.tiles, s.bars, s.scales, s.table, s.parts, s.end);
     }
 }
 """
-NAMES = "pair tmax tokens channels cut share part_buffers stages smem ctas tiles bars scales table parts end".split()
+NAMES = "wide tmax tokens channels cut share part_buffers stages smem ctas tiles bars scales table parts end".split()
 
 
 @pytest.fixture(scope="module")
@@ -43,8 +43,8 @@ def plan(tmp_path_factory):
 
 def _check(p, rows, experts, N, K, sms, grouped):
     kb = -(-K // 128)
-    if p["pair"]:
-        assert p["tokens"] == 256 and rows > 128
+    if p["wide"]:
+        assert p["tokens"] == 128 and rows > 64 and N > 128
         return
     assert p["tmax"] in (16, 32, 64, 128) and 16 <= p["tokens"] <= p["tmax"] and p["tokens"] % 16 == 0
     assert p["channels"] % 8 == 0 and 64 <= p["channels"] <= 128
@@ -86,18 +86,18 @@ def test_any_size_has_a_plan(plan):
     assert len(plans) == len(cases)
     for c, p in zip(cases, plans):
         _check(p, *c)
-    assert {p["cut"] for p in plans if not p["pair"]} == set(range(1, 9))
+    assert {p["cut"] for p in plans if not p["wide"]} == set(range(1, 9))
 
 
 def test_the_shapes_of_the_gpu_tests_reach_both_kernels(plan):
-    for shapes, pair in ((FEW, 0), (MANY, 1)):
+    for shapes, wide in ((FEW, 0), (MANY, 1)):
         for s, p in zip(shapes, plan([(M, 1, N, K, 148, 0) for M, N, K in shapes])):
-            assert p["pair"] == pair, s
+            assert p["wide"] == wide, s
     for counts in EXPERTS_FEW:
         for p in plan([(sum(counts) + 6, len(counts), N, K, 148, 1) for N, K in ((16, 16), (272, 400), (1408, 2048), (128, 4096))]):
-            assert p["pair"] == 0, counts
+            assert p["wide"] == 0, counts
     for counts in EXPERTS_MANY:
         for p in plan([(sum(counts) + 6, len(counts), N, K, 148, 1) for N, K in EXPERTS_MANY_LAYERS]):
-            assert p["pair"] == 1, counts
+            assert p["wide"] == 1, counts
     cuts = {p["cut"] for p in plan([(M, 1, N, K, 148, 0) for M, N, K in FEW])}
     assert {1, 2, 4, 5, 8} <= cuts, cuts
