@@ -56,7 +56,7 @@ class MoeMlpBlock:
         return self.gate_up.w8.shape[0]
 
     def forward(self, x, logits, out=None):
-        """x BF16 [M, H], logits BF16 or FP32 [M, E]; returns BF16 [M, H]."""
+        """x BF16 [M, H] of at least one token, logits BF16 or FP32 [M, E]; returns BF16 [M, H]."""
         if logits.shape[1] != self.experts or x.shape[0] != logits.shape[0]:
             raise ValueError("logits %s for %d tokens and %d experts" % (tuple(logits.shape), x.shape[0], self.experts))
         o = self.ops
