@@ -9,12 +9,12 @@
 // Nothing here is near the bound of its bytes (2 MB of logits: 0.4 us): what counts are launches and the length of the chain of
 // dependent steps of a token -- load, keys, groups, top_k rounds of a warp-wide maximum, weights.  Hence: a key carries its
 // expert's index in its low bits, so that no two are equal and a maximum says whose it is; a lane sorts its keys once and
-// gives up the first (looking for the next one among eight took 525 cycles a round, this takes 150); groups are judged all at
+// gives up the first (looking for the next one among eight took 525 cycles a round, this takes 150); groups are ranked all at
 // once by exchanges among the lanes that hold them; weights in FP64 for as many of a warp's tokens at a time as fill its lanes;
 // the next token's logits are fetched ahead.  Measured: 64 tokens of 256 experts in 8 groups 7.3 us, 8192 tokens of 128 experts
 // 17.3 us.
 //
-// The choice: without a bias and with groups judged by their best expert, scores have the order of the logits, whose 32 bits are
+// The choice: without a bias and with groups ranked by their best expert, scores have the order of the logits, whose 32 bits are
 // the keys' upper words.  Otherwise (WIDE) a key is score + bias in FP64, cut to 43 bits of fraction: in FP32 two experts whose
 // keys differ by less than a rounding would change places.
 #pragma once
@@ -280,7 +280,7 @@ route_choose_kernel(const RouteParams p) {
                 // A group's key: the sum of the group_best highest, lowest where one of them cannot be chosen.  (An index in its low
                 // bits does no harm: groups of equal value are taken in their order, which is that of their best experts' indices
                 // as long as these are not compared; so they are taken off.)
-                auto judge = [&](uint64_t top, uint64_t next) -> uint64_t {
+                auto group_key = [&](uint64_t top, uint64_t next) -> uint64_t {
                     if (WIDE && p.group_best == 2 && size > 1) return top == 0 || next == 0 ? 0 : order_bits(key_value(top) + key_value(next));
                     return top == 0 ? 0 : top | kRouteIndexBits;
                 };
@@ -296,7 +296,7 @@ route_choose_kernel(const RouteParams p) {
                         second = max64(max64(second, s2), min64(best, b2));
                         best = max64(best, b2);
                     }
-                    const uint64_t score = judge(best, second);
+                    const uint64_t score = group_key(best, second);
                     const int mine = lane / span;
                     int before = 0;   // groups that come before this lane's
 #pragma unroll 8
@@ -309,7 +309,7 @@ route_choose_kernel(const RouteParams p) {
                         for (int i = 0; i < V; ++i) key[i] = 0;
                     }
                 } else {
-                    uint64_t score = 0;   // lane g judges group g
+                    uint64_t score = 0;   // lane g has the key of group g
                     for (int g = 0; g < p.groups; ++g) {
                         uint64_t best = 0, second = 0;   // this lane's in the group
 #pragma unroll
@@ -319,7 +319,7 @@ route_choose_kernel(const RouteParams p) {
                             best = max64(best, key[i]);
                         }
                         const uint64_t top = warp_max(best), next = warp_max(best == top ? second : best);
-                        if (lane == g) score = judge(top, next);
+                        if (lane == g) score = group_key(top, next);
                     }
                     int before = 0;
                     for (int g = 0; g < p.groups; ++g) {
