@@ -24,16 +24,17 @@ __device__ __forceinline__ void block_scale(float amax, float& s, float& inv) {
 // Two values of g / (1 + exp(-g)) * u, two FP32 lanes per instruction where there is one: at 32 instructions a value the kernel was
 // bound by their issue ((4096, 14336) 72.6 us).  exp(-g) = 2^t (1 + l ln 2) with t = -g log2(e) rounded and l what the rounding took,
 // log2(e) in two parts; approximations of 2^t (2^-22) and of the reciprocal (2^-23), so that silu is within 2^-20.5.  Gates below -87
-// give 0: there the reciprocal is below the normal numbers.  A gate that is NaN or infinite gives NaN.
+// give 0: there the reciprocal is below the normal numbers.  t stays finite, so that l does for every finite gate (gates above 2.36e38
+// would have l = infinity, and 0 times it behind a 2^t of 0).  A gate that is NaN or infinite gives NaN.
 __device__ __forceinline__ unsigned long long silu_mul(float g0, float g1, float u0, float u1) {
     constexpr float c_hi = -1.44269502162933349609375f, c_lo = -1.92596299e-8f, ln2 = 0.69314718056f;
     const unsigned long long g = pack_f32x2(g0, g1), low = pack_f32x2(fmaxf(g0, -88.0f), fmaxf(g1, -88.0f));
-    const unsigned long long t = mul_f32x2(low, pack_f32x2(c_hi, c_hi));
     float t0, t1, e0, e1;
-    unpack_f32x2(t, t0, t1);
+    unpack_f32x2(mul_f32x2(low, pack_f32x2(c_hi, c_hi)), t0, t1);
+    t0 = fmaxf(t0, -3.402823466e38f), t1 = fmaxf(t1, -3.402823466e38f);
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
-    unsigned long long l = fma_f32x2(low, pack_f32x2(c_hi, c_hi), t ^ 0x8000000080000000ull);
+    unsigned long long l = fma_f32x2(low, pack_f32x2(c_hi, c_hi), pack_f32x2(-t0, -t1));
     l = fma_f32x2(low, pack_f32x2(c_lo, c_lo), l);
     const unsigned long long e = pack_f32x2(e0, e1);
     // 1 + e + e l ln 2
