@@ -142,14 +142,20 @@ quantize_blocks_kernel(const uint16_t* __restrict__ x, int M, int K, int64_t ldx
     }
 }
 
-// Eight consecutive values of a row as FP32.
+// Eight consecutive values of a row as FP32.  READ_ONLY: of memory that the kernel does not write.
+template <bool READ_ONLY>
 __device__ __forceinline__ void load8(const void* base, int64_t at, bool fp32, float (&v)[8]) {
     if (fp32) {
         const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-        const float4 a = __ldg(p), b = __ldg(p + 1);
+        float4 a, b;
+        if constexpr (READ_ONLY) a = __ldg(p), b = __ldg(p + 1);
+        else a = p[0], b = p[1];
         v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
     } else {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at));
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
+        uint4 a;
+        if constexpr (READ_ONLY) a = __ldg(p);
+        else a = *p;
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -165,12 +171,13 @@ __device__ __forceinline__ uint32_t bf16x2_bits(float lo, float hi) {
 }
 
 // out[m] = add[m] + sum_j weights[m][j] * y[slots[m][j]]: FP32 sums in ascending order of j behind the added row, rounded once.
-// A thread holds eight columns of a token; the rows of four experts are in flight at a time.
+// A thread holds eight columns of a token; the rows of four experts are in flight at a time.  `add` may be `out`: a thread reads its
+// piece of the one before it writes that of the other, and no thread reads another's.
 template <bool Y32, bool OUT32>
 __global__ void __launch_bounds__(256)
 combine_experts_kernel(const void* __restrict__ y, int64_t rows, int64_t ldy, const int32_t* __restrict__ slots,
-                       const float* __restrict__ weights, int64_t M, int top_k, int N, const void* __restrict__ add, int64_t ldadd,
-                       void* __restrict__ out, int64_t ldo) {
+                       const float* __restrict__ weights, int64_t M, int top_k, int N, const void* add, int64_t ldadd, void* out,
+                       int64_t ldo) {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const int per_row = N >> 3;
@@ -184,7 +191,7 @@ combine_experts_kernel(const void* __restrict__ y, int64_t rows, int64_t ldy, co
         }
         const int col = piece * 8;
         float acc[8] = {};
-        if (add != nullptr) load8(add, m * ldadd + col, OUT32, acc);
+        if (add != nullptr) load8<false>(add, m * ldadd + col, OUT32, acc);
         for (int j0 = 0; j0 < top_k; j0 += 4) {
             float v[4][8], w[4];
 #pragma unroll
@@ -193,7 +200,7 @@ combine_experts_kernel(const void* __restrict__ y, int64_t rows, int64_t ldy, co
                 const bool have = r >= 0 && r < rows;
                 w[j] = have ? __ldg(weights + m * top_k + j0 + j) : 0.0f;
                 if (have) {
-                    load8(y, r * ldy + col, Y32, v[j]);
+                    load8<true>(y, r * ldy + col, Y32, v[j]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
