@@ -623,118 +623,117 @@ linear_blocks_wide_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E
     const int first = (int)blockIdx.x, step = (int)gridDim.x, KB = p.KB;
     const int n_it = first < tiles ? ((tiles - first + step - 1) / step) * KB : 0;   // k-blocks of all tiles of this CTA
 
-    if (warp == 8) {
-        // ------------------------------------------------------------------ loads (whole warp, one lane issues)
-        // (registers: 64 x 128 + 216 x 256 threads of the 168 x 384 that the block is launched with)
+    // Registers: 64 x 128 + 216 x 256 threads of the 168 x 384 that the block is launched with.  setmaxnreg is one instruction for all four
+    // warps of a group, ahead of the roles in which they part.
+    if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        bool ok = true;
-        ptx::Ring r;
-        int issued = 0;
-        for (int i = first; i < tiles && ok; i += step) {
-            const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
-            for (int b = 0; b < KB; ++b) {
-                if (issued >= S) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+        if (warp == 8) {
+            // ------------------------------------------------------------------ loads (whole warp, one lane issues)
+            bool ok = true;
+            ptx::Ring r;
+            int issued = 0;
+            for (int i = first; i < tiles && ok; i += step) {
+                const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
+                for (int b = 0; b < KB; ++b) {
+                    if (issued >= S) ok = ptx::mbar_wait_warp(bar_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    const uint32_t full = bar_full + 8u * r.idx, dst = base + (uint32_t)r.idx * kStageBytes;
+                    if (ptx::elect_one()) {   // (channels and rows that are not there come as zeros)
+                        ptx::mbar_arrive_expect_tx(full, kStageBytes);
+                        ptx::tma_load_2d(dst, &tmap_x, b * 128, (int)t.row, full);
+                        ptx::tma_load_3d(dst + 16384u, &tmap_w, b * 128, t.nb * 128, t.e, full);
+                        ptx::tma_load_3d(dst + 32768u, &tmap_w, b * 128, t.nb * 128 + 128, t.e, full);
+                    }
+                    r.advance(S);
+                    ++issued;
+                }
+            }
+            if (!ok && lane == 0) {   // gave up: let the copies in flight land before the CTA goes away
+                const uint64_t t0 = ptx::globaltimer_ns();
+                for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+                    while (!ptx::mbar_try_wait(bar_full + 8u * (i % S), (uint32_t)((i / S) & 1)) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 20) {
+                    }
+            }
+            __syncwarp();
+        } else if (warp == 9) {
+            // ------------------------------------------------------------------ MMAs (whole warp, one lane issues)
+            constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(kWideTokens, 256);
+            bool ok = true;
+            ptx::Ring r, a;
+            for (int it = 0; it < n_it; ++it) {
+                // (the buffer is waited for last: it is what comes last)
+                ok = ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
+                if (it >= 2) ok = ok && ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
                 if (!ok) break;
-                const uint32_t full = bar_full + 8u * r.idx, dst = base + (uint32_t)r.idx * kStageBytes;
-                if (ptx::elect_one()) {   // (channels and rows that are not there come as zeros)
-                    ptx::mbar_arrive_expect_tx(full, kStageBytes);
-                    ptx::tma_load_2d(dst, &tmap_x, b * 128, (int)t.row, full);
-                    ptx::tma_load_3d(dst + 16384u, &tmap_w, b * 128, t.nb * 128, t.e, full);
-                    ptx::tma_load_3d(dst + 32768u, &tmap_w, b * 128, t.nb * 128 + 128, t.e, full);
+                ptx::tc_fence_after_sync();
+                const uint32_t s = base + (uint32_t)r.idx * kStageBytes;
+                const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
+                if (ptx::elect_one()) {
+                    ptx::umma_f8_kblock(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
+                    ptx::umma_commit(bar_acc + 8u * a.idx);
+                    ptx::umma_commit(bar_free + 8u * r.idx);
                 }
                 r.advance(S);
-                ++issued;
+                a.advance(2);
             }
-        }
-        if (!ok && lane == 0) {   // gave up: let the copies in flight land before the CTA goes away
-            const uint64_t t0 = ptx::globaltimer_ns();
-            for (int i = issued > S ? issued - S : 0; i < issued; ++i)
-                while (!ptx::mbar_try_wait(bar_full + 8u * (i % S), (uint32_t)((i / S) & 1)) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs / 20) {
+            if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
+                ptx::umma_commit(bar_drain);
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
                 }
-        }
-        __syncwarp();
-    } else if (warp == 9) {
-        // ------------------------------------------------------------------ MMAs (whole warp, one lane issues)
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        constexpr uint32_t idesc = ptx::umma_idesc_e4m3_f32(kWideTokens, 256);
-        bool ok = true;
-        ptx::Ring r, a;
-        for (int it = 0; it < n_it; ++it) {
-            // (the buffer is waited for last: it is what comes last)
-            ok = ptx::mbar_wait_warp(bar_full + 8u * r.idx, r.phase, abort_flag, p.status);
-            if (it >= 2) ok = ok && ptx::mbar_wait_warp(bar_acc_free + 8u * a.idx, a.phase ^ 1u, abort_flag, p.status);
-            if (!ok) break;
-            ptx::tc_fence_after_sync();
-            const uint32_t s = base + (uint32_t)r.idx * kStageBytes;
-            const uint32_t a_lo = ptx::umma_desc_lo(s), b_lo = ptx::umma_desc_lo(s + 16384u);
-            if (ptx::elect_one()) {
-                ptx::umma_f8_kblock(tmem + (uint32_t)(a.idx * 256), a_lo, b_lo, idesc, 0u);
-                ptx::umma_commit(bar_acc + 8u * a.idx);
-                ptx::umma_commit(bar_free + 8u * r.idx);
             }
-            r.advance(S);
-            a.advance(2);
-        }
-        if (!ok && lane == 0) {   // gave up: wait for the MMAs already issued before tensor memory is freed
-            ptx::umma_commit(bar_drain);
-            const uint64_t t0 = ptx::globaltimer_ns();
-            while (!ptx::mbar_try_wait(bar_drain, 0u) && ptx::globaltimer_ns() - t0 < ptx::kWaitLimitNs) {
-            }
-        }
-        __syncwarp();
-    } else if (warp == 10) {
-        // ------------------------------------------------------------------ scales (a lane has four tokens), and what the tiles are
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        bool ok = true;
-        ptx::Ring r;
-        int filled = 0, n = 0;
-        const bool wide = (p.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(p.s_x) & 15u) == 0;
-        for (int i = first; i < tiles && ok; i += step, ++n) {
-            const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
-            const float* sw0 = p.s_w + ((int64_t)t.e * p.NB + t.nb) * KB;
-            const float* sw1 = t.nb + 1 < p.NB ? sw0 + KB : sw0;
-            for (int b0 = 0; b0 < KB; b0 += kBlocksChunk) {
-                float w0 = 0.0f, w1 = 0.0f;
-                const int len = min(kBlocksChunk, KB - b0);
-                if (lane < len) {
-                    w0 = __ldg(sw0 + b0 + lane);
-                    w1 = __ldg(sw1 + b0 + lane);
-                }
-                if (filled >= 2) ok = ptx::mbar_wait_warp(bar_scales_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
-                if (!ok) break;
-                // (four places: the chunk of a tile that comes two tiles later waits for all warps to be done with this tile's)
-                if (b0 == 0 && lane == 0) ptx::st_shared_v4(tile_info + (uint32_t)((n & 3) * 16), make_uint4((uint32_t)t.row, (uint32_t)t.count, (uint32_t)t.nb, 0u));
-                float* f = reinterpret_cast<float*>(sm + kWideScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
-#pragma unroll 2
-                for (int k = 0; k < 4; ++k) {
-                    const int in = k * 32 + lane;
-                    const float* sx = p.s_x + (t.row + min(in, t.count - 1)) * p.lds + b0;   // (a row that exists)
-                    float x[kBlocksChunk];
-                    if (wide && len == kBlocksChunk) {
-                        const float4 u = __ldg(reinterpret_cast<const float4*>(sx)), v = __ldg(reinterpret_cast<const float4*>(sx) + 1);
-                        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < kBlocksChunk; ++j) x[j] = j < len ? __ldg(sx + j) : 0.0f;
+            __syncwarp();
+        } else if (warp == 10) {
+            // ------------------------------------------------------------------ scales (a lane has four tokens), and what the tiles are
+            bool ok = true;
+            ptx::Ring r;
+            int filled = 0, n = 0;
+            const bool wide = (p.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(p.s_x) & 15u) == 0;
+            for (int i = first; i < tiles && ok; i += step, ++n) {
+                const BlocksTile t = wide_blocks_tile(p, table, i, token_tiles);
+                const float* sw0 = p.s_w + ((int64_t)t.e * p.NB + t.nb) * KB;
+                const float* sw1 = t.nb + 1 < p.NB ? sw0 + KB : sw0;
+                for (int b0 = 0; b0 < KB; b0 += kBlocksChunk) {
+                    float w0 = 0.0f, w1 = 0.0f;
+                    const int len = min(kBlocksChunk, KB - b0);
+                    if (lane < len) {
+                        w0 = __ldg(sw0 + b0 + lane);
+                        w1 = __ldg(sw1 + b0 + lane);
                     }
-#pragma unroll
-                    for (int j = 0; j < kBlocksChunk; ++j) {
-                        f[j * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w0, j);
-                        f[(kBlocksChunk + j) * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w1, j);
+                    if (filled >= 2) ok = ptx::mbar_wait_warp(bar_scales_free + 8u * r.idx, r.phase ^ 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    // (four places: the chunk of a tile that comes two tiles later waits for all warps to be done with this tile's)
+                    if (b0 == 0 && lane == 0) ptx::st_shared_v4(tile_info + (uint32_t)((n & 3) * 16), make_uint4((uint32_t)t.row, (uint32_t)t.count, (uint32_t)t.nb, 0u));
+                    float* f = reinterpret_cast<float*>(sm + kWideScales) + r.idx * 2 * kBlocksChunk * 128 + lane;
+    #pragma unroll 2
+                    for (int k = 0; k < 4; ++k) {
+                        const int in = k * 32 + lane;
+                        const float* sx = p.s_x + (t.row + min(in, t.count - 1)) * p.lds + b0;   // (a row that exists)
+                        float x[kBlocksChunk];
+                        if (wide && len == kBlocksChunk) {
+                            const float4 u = __ldg(reinterpret_cast<const float4*>(sx)), v = __ldg(reinterpret_cast<const float4*>(sx) + 1);
+                            x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+                        } else {
+    #pragma unroll
+                            for (int j = 0; j < kBlocksChunk; ++j) x[j] = j < len ? __ldg(sx + j) : 0.0f;
+                        }
+    #pragma unroll
+                        for (int j = 0; j < kBlocksChunk; ++j) {
+                            f[j * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w0, j);
+                            f[(kBlocksChunk + j) * 128 + k * 32] = x[j] * __shfl_sync(0xFFFFFFFFu, w1, j);
+                        }
                     }
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar_scales + 8u * r.idx);
+                    r.advance(2);
+                    ++filled;
                 }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar_scales + 8u * r.idx);
-                r.advance(2);
-                ++filled;
             }
+            __syncwarp();
         }
-        __syncwarp();
-    } else if (warp == 11) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     } else {
-        // ------------------------------------------------------------------ sums and outputs: thread = token
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // ------------------------------------------------------------------ sums and outputs: thread = token
         // (128 registers of sums and 64 of columns leave few: the loop over k-blocks keeps next to nothing, and what is needed
         // around it is read again.  With spills in it, it took a third longer; with the tile worked out twice by each of these warps,
         // it took 8 % longer for 32768 rows of 64 experts of (4096, 2048).)
