@@ -536,8 +536,9 @@ int w4a8_linear_fp8_experts(const uint8_t* x8, int64_t ldx8, const float* s_x, i
  *   smaller group; only experts of the top_groups groups of highest key can be chosen;
  *   the top_k experts of highest key are chosen in descending order.  Equal keys: the lower index first, groups and experts.
  *   weights = score, divided by the sum of the chosen scores (renormalize = 1; 0 where that sum is 0), times scale.
- * Scores and weights are evaluated in FP64 and rounded once -- but the sum of a softmax over all experts, which only renormalize = 0
- * needs, in FP32 where keys are compared as logits (next sentence): such weights are within (E / 32 + 17) 2^-24 of theirs.
+ * Scores and weights are evaluated in FP64 (a sigmoid has fewer bits for logits below -708 and is 0 below -745) and rounded once --
+ * but the sum of a softmax over all experts, which only renormalize = 0 needs, in FP32 where keys are compared as logits (next
+ * sentence): such weights are within (E / 32 + 17) 2^-24 of theirs.
  * Without a bias and with one group or group_best = 1 keys are compared as the logits themselves, which have their order.
  * Otherwise as FP64 values without the last 9 bits: keys that agree in their first 44 bits count as equal.
  * Experts whose logit is NaN or -inf, or whose bias is, cannot be chosen (a NaN logit counts as -inf in the softmax); a group with

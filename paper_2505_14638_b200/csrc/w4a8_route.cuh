@@ -126,13 +126,13 @@ __device__ __forceinline__ double plain_exp(double t) {
     const int half = n >> 1;
     return v * __hiloint2double((1023 + half) << 20, 0) * __hiloint2double((1023 + n - half) << 20, 0);
 }
-// d from 1 to infinity: an approximation of 20 bits, and two of Newton's steps.
+// d from 1 to 2: an approximation of 20 bits, and two of Newton's steps.
 __device__ __forceinline__ double plain_inverse(double d) {
     double y;
     asm("rcp.approx.ftz.f64 %0, %1;" : "=d"(y) : "d"(d));
     y = fma(y, fma(-d, y, 1.0), y);
     y = fma(y, fma(-d, y, 1.0), y);
-    return d > 1e300 ? 0.0 : y;
+    return y;
 }
 
 // Row offsets of the experts from their counts, exclusive, by all warps (one of them per 32 experts); `sums`: a word per warp.
@@ -243,7 +243,9 @@ route_choose_kernel(const RouteParams p) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     if (p.sigmoid) {
-                        s[i] = plain_inverse(1.0 + plain_exp((double)fminf(fmaxf(-x[i], -1000.0f), 1000.0f)));
+                        // (of exp(-|x|), so that scores keep their order down to FP64's least number, logits of -745)
+                        const double z = plain_exp(fmax(-fabs((double)x[i]), -1000.0)), of_positive = plain_inverse(1.0 + z);
+                        s[i] = x[i] < 0.0f ? z * of_positive : of_positive;
                     } else {
                         s[i] = x[i] == most ? 1.0 : plain_exp(fmax((double)x[i] - (double)most, -1000.0));   // (0 where x is -inf)
                         sum64 += s[i];
@@ -356,7 +358,12 @@ route_choose_kernel(const RouteParams p) {
         double w = 0.0;
         if (id >= 0) {
             const double v = (double)route_logit(p, m * p.ldl + id);
-            w = p.sigmoid ? 1.0 / (1.0 + exp(-v)) : route_exp(v, (double)most_mine);
+            if (p.sigmoid) {
+                const double z = exp(-fabs(v));
+                w = (v < 0.0 ? z : 1.0) / (1.0 + z);
+            } else {
+                w = route_exp(v, (double)most_mine);
+            }
         }
         double by = p.sigmoid ? 1.0 : sum_mine;
         if (p.renormalize) {
