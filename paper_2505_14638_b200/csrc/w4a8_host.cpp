@@ -147,6 +147,9 @@ int run_on(const at::Tensor& t, F f) {
     return rc;
 }
 
+// From row to row; of a single one (whose stride PyTorch leaves open) its width.
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+
 int64_t blocks_of(int64_t n) { return (n + 127) / 128; }
 
 // (x, input_kind, slots or None, x8, s_x) -> status
@@ -169,8 +172,8 @@ PyObject* quantize_act_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
             top_k = static_cast<int>(t.size(1));
         }
         return run_on(x, [&](void* stream) {
-            return w4a8_quantize_act_blocks(x.data_ptr(), x.size(0), K, x.stride(0), kind, slots, top_k, static_cast<uint8_t*>(x8.data_ptr()),
-                                            x8.size(0), x8.stride(0), static_cast<float*>(s_x.data_ptr()), s_x.stride(0), stream);
+            return w4a8_quantize_act_blocks(x.data_ptr(), x.size(0), K, row_stride(x), kind, slots, top_k, static_cast<uint8_t*>(x8.data_ptr()),
+                                            x8.size(0), row_stride(x8), static_cast<float*>(s_x.data_ptr()), row_stride(s_x), stream);
         });
     });
 }
@@ -198,15 +201,16 @@ PyObject* linear_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float *sx = static_cast<const float*>(s_x.data_ptr()), *sw = static_cast<const float*>(s_w.data_ptr());
         if (!experts)
             return run_on(x8, [&](void* stream) {
-                return w4a8_linear_fp8_blocks(xp, x8.stride(0), sx, s_x.stride(0), M, wp, w8.stride(0), sw, N, K, out.data_ptr(),
-                                              out.stride(0), od, stream);
+                return w4a8_linear_fp8_blocks(xp, row_stride(x8), sx, row_stride(s_x), M, wp, row_stride(w8), sw, N, K, out.data_ptr(),
+                                              row_stride(out), od, stream);
             });
         const at::Tensor& offsets = on_device(a[2], "offsets", at::kInt, 1);
         check(offsets.size(0) == E + 1, "offsets: [experts + 1]");
         same_device(x8, offsets);
+        const int64_t ldw = w8.stride(1), w_stride = E > 1 ? w8.stride(0) : N * ldw;
         return run_on(x8, [&](void* stream) {
-            return w4a8_linear_fp8_experts(xp, x8.stride(0), sx, s_x.stride(0), M, static_cast<const int32_t*>(offsets.data_ptr()), E, wp,
-                                           w8.stride(1), w8.stride(0), sw, N, K, out.data_ptr(), out.stride(0), od, stream);
+            return w4a8_linear_fp8_experts(xp, row_stride(x8), sx, row_stride(s_x), M, static_cast<const int32_t*>(offsets.data_ptr()), E, wp,
+                                           ldw, w_stride, sw, N, K, out.data_ptr(), row_stride(out), od, stream);
         });
     });
 }
@@ -246,7 +250,7 @@ PyObject* route_experts(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const double scale = PyFloat_AsDouble(a[7]);
         if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
         return run_on(logits, [&](void* stream) {
-            return w4a8_route_experts(logits.data_ptr(), dtype, M, logits.stride(0), E, static_cast<int>(k), score, bias, groups, top_groups, best,
+            return w4a8_route_experts(logits.data_ptr(), dtype, M, row_stride(logits), E, static_cast<int>(k), score, bias, groups, top_groups, best,
                                       renormalize, static_cast<float>(scale), static_cast<int32_t*>(ids.data_ptr()),
                                       static_cast<float*>(weights.data_ptr()), static_cast<int32_t*>(offsets.data_ptr()),
                                       static_cast<int32_t*>(slots.data_ptr()), ws, wsn, stream);
@@ -270,15 +274,15 @@ PyObject* combine_experts(PyObject*, PyObject* const* a, Py_ssize_t n) {
             check(dtype_of(a[3], "add", 2) == od && t.sizes() == out.sizes(), "add: of the shape and type of the result");
             same_device(y, t);
             add = t.data_ptr();
-            ldadd = t.stride(0);
+            ldadd = row_stride(t);
         }
         same_device(y, slots);
         same_device(y, weights);
         same_device(y, out);
         return run_on(y, [&](void* stream) {
-            return w4a8_combine_experts(y.data_ptr(), yd, y.size(0), y.stride(0), static_cast<const int32_t*>(slots.data_ptr()),
+            return w4a8_combine_experts(y.data_ptr(), yd, y.size(0), row_stride(y), static_cast<const int32_t*>(slots.data_ptr()),
                                         static_cast<const float*>(weights.data_ptr()), M, static_cast<int>(slots.size(1)), N, add, ldadd,
-                                        out.data_ptr(), out.stride(0), od, stream);
+                                        out.data_ptr(), row_stride(out), od, stream);
         });
     });
 }
