@@ -1,7 +1,7 @@
 // Activations to E4M3 with one scale per token and block of 128 columns (plain or gated, optionally written to the rows that
 // the experts of each token read), and the weighted sum of the experts' outputs of each token.  Both are bound by HBM: (4096, 14336)
-// gated 47.4 us (295 MB: 6.2 TB/s), the sum of 8 rows of 4096 values for each of 4096 tokens 49.4 us (302 MB: 6.1 TB/s); a few
-// tokens take a launch, 2.2 us.
+// gated 47.4 us in a graph (295 MB: 6.2 TB/s) and 48 to 55 as calls, the sum of 8 rows of 4096 values for each of 4096 tokens 49.7 us
+// in a graph (302 MB: 6.1 TB/s) and 51.3 as calls; a few tokens take a launch, 2.2 us.
 #pragma once
 
 #include <cuda_bf16.h>

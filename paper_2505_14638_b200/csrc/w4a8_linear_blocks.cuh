@@ -20,10 +20,11 @@
 // Warps: 0 loads, 1 MMAs (and tensor memory's allocation), 2 and 3 outputs, then one group of four that adds, or two above 32 tokens
 // (each half of the tokens: with one, 80 tokens were bound by it, 780 cycles a k-block).
 //
-// Measured: 512 rows of 120 of 128 experts, (4096, 4096) each (2.0 GB of weights), 290 us: 7.0 TB/s, more than a plain copy reaches
+// Measured: 512 rows of 120 of 128 experts, (4096, 4096) each (2.0 GB of weights), 289 to 302 us: 6.7 to 7.0 TB/s, more than a plain copy reaches
 // (reads alone).  128 rows of 31 experts 102 us: DRAM reads are the weights' 521 MB, once.  Few weights are bound by what surrounds
-// their stream -- launch, first loads, the sums' way, outputs: (77, 14336, 4096) 18.8 us, 3.1 TB/s; (1, 6144, 4096) 8.0 us, 3.1
-// TB/s; 8 rows of 8 experts 13.3 us, 3.5 TB/s.  Asking for the first weights ahead of the wait for the earlier kernel gained nothing.
+// their stream -- launch, first loads, the sums' way, outputs: (77, 14336, 4096) 19.4 us, 3.3 TB/s (of its tiles' 80 tokens the first
+// group that adds has 64); (1, 6144, 4096) 7.5 us, 3.3 TB/s; 8 rows of 8 experts 13.6 us, 3.4 TB/s.  Asking for the first weights ahead
+// of the wait for the earlier kernel gained nothing.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -532,11 +533,13 @@ linear_blocks_kernel(const __grid_constant__ CUtensorMap tmap_w,   // w8 [E][N][
 //
 // Bound by that exchange of the buffers -- a k-block's 512 cycles, then the way from the MMAs' completion to the warps that add, their
 // fetch and the way back, of which only a part hides behind the other buffer's MMAs; tensor memory holds no third one of 256 columns --
-// and, where a launch lasts, by the power limit.  (2048, 8192, 8192) 146 us, 1.9 PFLOP/s; (8192, 8192, 4096) 264 us, 2.1 PFLOP/s;
-// (8192, 28672, 8192) 1970 us, 1.95 PFLOP/s, at 1.1 to 1.3 GHz.  Tiles of 256 x 256 on pairs of CTAs, each with half of the channels'
-// weights, load two thirds of this, but their buffers' way back leads through the other CTA, and experts fill them worse: 158, 282 and
-// 2190 us; 64 experts of (4096, 2048) with 512 rows each 379 us instead of 334, with 128 rows 186 instead of 134.  Without gain on
-// pairs: sixteen warps that add, buffers of 128 columns, a second warp that issues, the first columns of the next k-block fetched ahead.
+// and, where a launch lasts, by the power limit.  On different GPUs (2048, 8192, 8192) 136 to 146 us, 1.9 to 2.0 PFLOP/s; (8192, 8192,
+// 4096) 254 to 264 us, 2.1 PFLOP/s; (8192, 28672, 8192) 1970 to 2180 us, 1.75 to 1.95 PFLOP/s, at 1.1 to 1.4 GHz, and 1650 to 1980 with
+// weights of zeros, which draw little power: the exchange comes first.  Tiles of 256 x 256 on pairs of CTAs, each with half of the
+// channels' weights, load two thirds of this, but their buffers' way back leads through the other CTA, and experts fill them worse, on
+// one GPU: 158 us instead of 146, 282 instead of 264, 2190 instead of 1970; 64 experts of (4096, 2048) with 512 rows each 379 instead of
+// 334, with 128 rows each 186 instead of 134.  Without gain on pairs, and not tried on single CTAs: sixteen warps that add, buffers of
+// 128 columns, a second warp that issues, the first columns of the next k-block fetched ahead.
 //
 // Warps: 0..7 sums and outputs (warp % 4 = lane quarter, warp / 4 = 128 of the channels), 8 loads, 9 MMAs, 10 scales (11 idle): the
 // products s_x * s_w of eight k-blocks at a time, through shared memory.  (Fetched by the warps that add, a k-block's scales cost

@@ -12,7 +12,7 @@
 // gives up the first (looking for the next one among eight took 525 cycles a round, this takes 150); groups are ranked all at
 // once by exchanges among the lanes that hold them; weights in FP64 (but for one sum, see there) for as many of a warp's tokens at a
 // time as fill its lanes; the next token's logits are fetched ahead.  Measured: 64 tokens of 256 experts in 8 groups 7.3 us, 8192
-// tokens of 128 experts 17.3 us.
+// tokens of 128 experts 16.4 to 19.4 us on different GPUs.
 //
 // The choice: without a bias and with groups ranked by their best expert, scores have the order of the logits, whose 32 bits are
 // the keys' upper words.  Otherwise (WIDE) a key is score + bias in FP64, cut to 43 bits of fraction: in FP32 two experts whose
@@ -29,7 +29,9 @@ namespace w4a8 {
 constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 32, kRouteMaxGroups = 32;
 constexpr int kRouteWarps = 16;      // tokens that a CTA works on at a time
 constexpr int kRouteCluster = 8;
-constexpr int kRouteChunks = 256;    // CTAs at most: 32 clusters are resident at two CTAs per SM, 36 took a second round
+// CTAs at most: 32 clusters are resident at two CTAs per SM, 36 took a second round.  Two CTAs per SM hold up to 128 experts; above,
+// 98 to 128 registers of 512 threads leave one, and 256 CTAs are two rounds (4096 tokens of 256 experts in 8 groups 31.7 us).
+constexpr int kRouteChunks = 256;
 constexpr int kRouteLocalIds = 2048; // choices of a CTA that are kept in shared memory
 
 struct RouteParams {
